@@ -346,6 +346,42 @@ cat_status_t cat_apply_pca(const float *Yq, int64_t N, int32_t D, int32_t K, int
                            const float *gamma, const float *beta, float *Y_out, int32_t *labels_out,
                            void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- the rows' makers and users: a layer's product, drafted tokens ------ */
+
+/* Element types of the entry points below (all others take fp32). */
+#define CAT_F32 0
+#define CAT_BF16 1
+#define CAT_F16 2
+
+/*
+ * A layer's matrix product with what follows it in one kernel -- the head whose rows cat_fit and cat_apply take, or any
+ * layer before it:
+ *   Y[i,:] = act(X[i,:] W^T + bias) + residual[i,:]            (i < M; W is [N, K], row n the weights of output column n)
+ * X [M, K] and W [N, K] are of in_type, CAT_BF16 or CAT_F16; Y [M, N] and residual [M, N] of out_type (any of the three);
+ * bias [N] of bias_type, may be NULL; residual may be NULL, or Y itself (with ldr = ldy; no other overlap).
+ * Rows are ldx, ldw, ldr, ldy elements apart (at least K, K, N, N; with one row its distance is not looked at); no base
+ * address needs more alignment than its element.  Products and sums are formed in fp32 on the tensor cores, bias, activation and residual in
+ * fp32 behind them, and the result is rounded once to out_type (overflow of fp16 gives infinities).  Non-finite inputs
+ * propagate as the arithmetic has it.  Activations:
+ *   CAT_ACT_RELU       max(z, 0)                     CAT_ACT_GELU       z Phi(z) (erf form)
+ *   CAT_ACT_GELU_TANH  z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2          CAT_ACT_SILU  z / (1 + e^-z)
+ * Results do not vary from run to run.  M = 0 does nothing.  Limits: M <= CAT_LINEAR_MAX_M, N and K <= CAT_LINEAR_MAX_N.
+ * Workspace: a control block; and where rows of X or W do not start on 16-byte boundaries (base or row distance), a copy
+ * of that matrix is made there in every call.  A program that keeps weights for many calls keeps them with ldw a
+ * multiple of 8.  The query only looks at the addresses.
+ */
+#define CAT_ACT_NONE 0
+#define CAT_ACT_RELU 1
+#define CAT_ACT_GELU 2
+#define CAT_ACT_GELU_TANH 3
+#define CAT_ACT_SILU 4
+#define CAT_LINEAR_MAX_M (1 << 24)
+#define CAT_LINEAR_MAX_N (1 << 20)
+size_t cat_linear_workspace_bytes(const void *X, int64_t ldx, const void *W, int64_t ldw, int64_t M, int32_t N, int32_t K);
+cat_status_t cat_linear(const void *X, int64_t ldx, const void *W, int64_t ldw, int32_t in_type, const void *bias, int32_t bias_type,
+                        const void *residual, int64_t ldr, int32_t activation, int64_t M, int32_t N, int32_t K,
+                        void *Y, int64_t ldy, int32_t out_type, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- host-buffer entry points (end-to-end use) ------------------------- */
 
 /*

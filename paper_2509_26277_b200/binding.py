@@ -38,6 +38,7 @@ EXPORTS = [
     "cat_fit_shard_begin", "cat_fit_shard_round", "cat_fit_shard_update",
     "cat_pca_workspace_bytes", "cat_pca_fit", "cat_pca_project", "cat_affine_with_labels",
     "cat_fit_pca_workspace_bytes", "cat_fit_pca", "cat_apply_pca_workspace_bytes", "cat_apply_pca",
+    "cat_linear_workspace_bytes", "cat_linear",
     "cat_centroids_from_sums",
     "cat_centred_moments", "cat_solve_gamma_beta", "cat_apply_host_workspace_bytes",
     "cat_apply_host", "cat_fit_host_workspace_bytes", "cat_fit_host", "cat_workspace_report",
@@ -127,6 +128,10 @@ def lib():
                  "cat_cluster_sums", "cat_centroids_from_sums", "cat_centred_moments",
                  "cat_solve_gamma_beta", "cat_apply_host", "cat_fit_host"):
         getattr(L, name).restype = ctypes.c_int
+    L.cat_linear_workspace_bytes.argtypes = [vp, i64, vp, i64, i64, i32, i32]
+    L.cat_linear_workspace_bytes.restype = sz
+    L.cat_linear.argtypes = [vp, i64, vp, i64, i32, vp, i32, vp, i64, i32, i64, i32, i32, vp, i64, i32, vp, sz, vp]
+    L.cat_linear.restype = ctypes.c_int
     L.cat_selftest_wait_timeout.argtypes = [vp, sz, i32, vp]
     L.cat_selftest_wait_timeout.restype = ctypes.c_int
     L.cat_workspace_report.argtypes = [vp, vp, vp, vp, vp]
@@ -511,6 +516,92 @@ def cat_solve_gamma_beta(sumQ, sumF, var_sum, cov_sum, counts):
                                     _dev(gamma, torch.float32), _dev(beta, torch.float32), _stream())
     _check(st, "cat_solve_gamma_beta")
     return gamma, beta
+
+
+# ---------------------------------------------------------------- the rows' makers and users
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}                       # CAT_F32, CAT_BF16, CAT_F16
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}             # CAT_ACT_*
+_control_blocks = {}
+
+
+def _call_on(device: torch.device, call):
+    """call(raw stream) with `device` current and its current stream (the library launches on the current device)."""
+    if device.index == torch.cuda.current_device():
+        return call(torch._C._cuda_getCurrentRawStream(device.index))
+    with torch.cuda.device(device):
+        return call(torch._C._cuda_getCurrentRawStream(device.index))
+
+
+def _control_block(device: torch.device, stream: int) -> torch.Tensor:
+    """The 256-byte workspace of the calls that need no more, one per stream (cat_workspace_report reads it)."""
+    ws = _control_blocks.get((device.index, stream))
+    if ws is None:
+        ws = _control_blocks[(device.index, stream)] = torch.empty(256, dtype=torch.uint8, device=device)
+    return ws
+
+
+def _matrix(t: torch.Tensor, name: str, device: torch.device, rows: int, cols: int) -> int:
+    """Distance of the rows of a 2-D device matrix whose columns are contiguous."""
+    if t.device != device:
+        raise TypeError(f"{name} must be a CUDA tensor on {device}, not on {t.device}")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{name} must have shape {(rows, cols)}, got {tuple(t.shape)}")
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return ld
+
+
+def cat_linear(X, W, bias=None, residual=None, activation: str = "none", out=None, out_dtype=None, ws=None):
+    """cat_linear: act(X W^T + bias) + residual for X [M, K] and W [N, K] in bf16 or fp16, [M, N] of out_dtype (default:
+    X's; residual's and out's type has to be the same).  Rows may be any distance apart."""
+    device = X.device
+    if device.type != "cuda":
+        raise TypeError("X must be a CUDA tensor")
+    if X.dim() != 2 or W.dim() != 2:
+        raise ValueError("X and W must be matrices")
+    M, K = X.shape
+    N = W.shape[0]
+    in_type = _TYPES.get(X.dtype, 0)
+    if in_type == 0 or W.dtype != X.dtype:
+        raise TypeError(f"X and W must both be bf16 or both fp16, got {X.dtype} and {W.dtype}")
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")
+    ldx, ldw = _matrix(X, "X", device, M, K), _matrix(W, "W", device, N, K)
+    if out is None:
+        out = torch.empty((M, N), dtype=out_dtype or X.dtype, device=device)
+    elif out_dtype is not None and out.dtype != out_dtype:
+        raise TypeError(f"out must be {out_dtype}, got {out.dtype}")
+    if out.dtype not in _TYPES:
+        raise TypeError(f"out must be fp32, bf16 or fp16, got {out.dtype}")
+    ldy, ldr = _matrix(out, "out", device, M, N), 0
+    if residual is not None:
+        ldr = _matrix(residual, "residual", device, M, N)
+        if residual.dtype != out.dtype:
+            raise TypeError(f"residual must be {out.dtype} as the output is, got {residual.dtype}")
+    if bias is not None:
+        if bias.device != device or bias.dtype not in _TYPES:
+            raise TypeError(f"bias must be fp32, bf16 or fp16 on {device}")
+        if bias.shape != (N,) or not bias.is_contiguous():
+            raise ValueError(f"bias must be contiguous of shape {(N,)}")
+    L = lib()
+    x, w = X.data_ptr(), W.data_ptr()
+
+    def call(stream):
+        room = ws
+        if room is None:
+            if (x | w) & 15 or (M > 1 and ldx & 7) or (N > 1 and ldw & 7):   # (copies of rows that the kernel cannot address)
+                room = torch.empty(max(256, L.cat_linear_workspace_bytes(x, ldx, w, ldw, M, N, K)), dtype=torch.uint8, device=device)
+            else:
+                room = _control_block(device, stream)
+        return L.cat_linear(x, ldx, w, ldw, in_type, bias.data_ptr() if bias is not None else None,
+                            _TYPES[bias.dtype] if bias is not None else 0, residual.data_ptr() if residual is not None else None, ldr,
+                            ACTIVATIONS[activation], M, N, K, out.data_ptr(), ldy, _TYPES[out.dtype], room.data_ptr(),
+                            room.numel() * room.element_size(), stream)
+
+    _check(_call_on(device, call), "cat_linear")
+    return out
 
 
 def cat_apply_host(Yq_host, centroids_host, gamma_host, beta_host, out_host, labels_host=None,

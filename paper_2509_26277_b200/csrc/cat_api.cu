@@ -835,6 +835,47 @@ cat_status_t cat_solve_gamma_beta(const double *sumQ, const double *sumF, const 
     return CAT_OK;
 }
 
+static bool is_type(int32_t t) { return t == CAT_F32 || t == CAT_BF16 || t == CAT_F16; }
+static bool misaligned(const void *p, int32_t type) { return reinterpret_cast<uintptr_t>(p) & (type == CAT_F32 ? 3u : 1u); }
+
+// (the distance of the only row of a matrix says nothing)
+static int64_t row_distance(int64_t ld, int64_t rows, int32_t K) { return rows > 1 ? ld : ((int64_t)K + 7) & ~(int64_t)7; }
+
+static cat_status_t check_linear(int64_t ldx, int64_t ldw, int64_t M, int32_t N, int32_t K)
+{
+    if (M < 0 || N < 1 || K < 1 || (M > 1 && ldx < K) || (N > 1 && ldw < K)) return CAT_ERR_SHAPE;
+    if (M > CAT_LINEAR_MAX_M || N > CAT_LINEAR_MAX_N || K > CAT_LINEAR_MAX_N) return CAT_ERR_UNSUPPORTED;
+    if ((M > 1 && ldx > INT32_MAX) || (N > 1 && ldw > INT32_MAX)) return CAT_ERR_UNSUPPORTED;
+    return CAT_OK;
+}
+
+size_t cat_linear_workspace_bytes(const void *X, int64_t ldx, const void *W, int64_t ldw, int64_t M, int32_t N, int32_t K)
+{
+    if (check_linear(ldx, ldw, M, N, K) != CAT_OK) return 0;
+    return linear_workspace_bytes(X, row_distance(ldx, M, K), W, row_distance(ldw, N, K), M, N, K);
+}
+
+cat_status_t cat_linear(const void *X, int64_t ldx, const void *W, int64_t ldw, int32_t in_type, const void *bias, int32_t bias_type,
+                        const void *residual, int64_t ldr, int32_t activation, int64_t M, int32_t N, int32_t K,
+                        void *Y, int64_t ldy, int32_t out_type, void *workspace, size_t workspace_bytes, void *stream)
+{
+    cat_status_t st = check_linear(ldx, ldw, M, N, K);
+    if (st != CAT_OK) return st;
+    if ((in_type != CAT_BF16 && in_type != CAT_F16) || !is_type(out_type) || (bias && !is_type(bias_type))) return CAT_ERR_SHAPE;
+    if (activation < CAT_ACT_NONE || activation > CAT_ACT_SILU) return CAT_ERR_SHAPE;
+    if (M > 1 && (ldy < N || (residual && ldr < N))) return CAT_ERR_SHAPE;
+    if (M > 1 && residual == Y && residual && ldr != ldy) return CAT_ERR_SHAPE;
+    if (M == 0) return CAT_OK;
+    if (!X || !W || !Y) return CAT_ERR_NULL;
+    if (misaligned(X, in_type) || misaligned(W, in_type) || misaligned(Y, out_type) || (residual && misaligned(residual, out_type)) ||
+        (bias && misaligned(bias, bias_type)))
+        return CAT_ERR_ALIGN;
+    LinearArgs a{X, W, bias, residual, Y, row_distance(ldx, M, K), row_distance(ldw, N, K), ldr, ldy, M, N, K, in_type, bias_type, out_type, activation};
+    if (!workspace || !aligned16(workspace) || workspace_bytes < linear_workspace_bytes(X, a.ldx, W, a.ldw, M, N, K)) return CAT_ERR_WORKSPACE;
+    CAT_CUDA(launch_linear(a, workspace, reinterpret_cast<cudaStream_t>(stream)));
+    return CAT_OK;
+}
+
 cat_status_t cat_workspace_report(const void *workspace, void *stream, int64_t *refined_last_host,
                                   int64_t *refined_total_host, int32_t *device_status_host)
 {

@@ -385,4 +385,14 @@ size_t sym_eig_workspace_bytes(int D, int p);
 cudaError_t launch_sym_eig(double *A, const double *diag, double *refl, int D, int p, float *comps, double *eig_out,
                            Control *ctl, void *workspace, cudaStream_t s);
 
+// Y = act(X W^T + b) + R (cat_linear.cu); fields as in cat.h, the row distances of one-row matrices already set to a multiple of 8.
+struct LinearArgs {
+    const void *X, *W, *bias, *residual;
+    void *Y;
+    int64_t ldx, ldw, ldr, ldy, M;
+    int32_t N, K, in_type, bias_type, out_type, act;
+};
+size_t linear_workspace_bytes(const void *X, int64_t ldx, const void *W, int64_t ldw, int64_t M, int N, int K);
+cudaError_t launch_linear(const LinearArgs &a, void *workspace, cudaStream_t s);
+
 }  // namespace cat

@@ -1,0 +1,510 @@
+// A layer's matrix product with what follows it, Y = act(X W^T + b) + R, in one kernel (cat_linear).
+//
+// Mathematics.  acc[n][t] = sum_k W[n][k] X[t][k] on the 5th-generation tensor cores (operands bf16 or fp16, products exact, sums in
+// fp32 in TMEM); z = acc + b[n], y = act(z) + R[t][n] in fp32, rounded once to the type of Y.
+//
+// Layout.  The rows of W take the 128 lanes of an accumulator and the tokens its columns, whatever the number of tokens: one token fills
+// an accumulator of 16 columns, and a thread of the epilogue owns one output column n -- its bias is one register, and the 32 lanes of a
+// warp write 32 neighbouring columns of Y, so outputs, strides and residuals need no alignment at all.  Both operands arrive by TMA in
+// 64-column slabs (128-byte swizzle, zero fill past the matrix, so K, N and M may be anything); rows that TMA cannot address (stride or base
+// not a multiple of 16 bytes) are copied to the workspace first.
+//
+// Forms.  Many tokens: CTA pairs (cta_group::2) on tiles of 256 columns of Y x up to 256 tokens, persistent, accumulators double buffered so
+// that one tile's epilogue passes under the next one's MMAs.  Few tokens: one CTA per 128 columns, and where those leave SMs idle the inner
+// dimension is split over the CTAs of a cluster, whose partial sums meet in distributed shared memory in a fixed order (no atomics: the
+// same call gives the same bits).
+#include "cat_tc.cuh"
+
+#include <cuda_bf16.h>
+
+namespace cat {
+namespace {
+
+constexpr int LN_BK = 64;                       // inner columns per slab (128 bytes)
+constexpr int LN_MAX_STAGES = 12;
+constexpr int LN_EPI_WARPS = 8;                 // two per quarter of the TMEM lanes
+constexpr int LN_THREADS = 32 * (2 + LN_EPI_WARPS);
+constexpr int LN_GROUP = 8;                     // token tiles that share a sweep over the weights
+
+struct LinearParams {
+    const void *bias;
+    const void *residual;
+    void *Y;
+    Control *ctl;
+    int64_t ldr, ldy;
+    int64_t M;
+    int N, K;
+    int nt;            // tokens per tile
+    int nt_cta;        // of which this CTA stages that many
+    int tiles_w;       // tiles along N
+    int tiles_t;       // tiles along M
+    int splits;        // CTAs of a cluster that share a tile's inner dimension (1: none)
+    int stages;
+    int tmem_cols;
+    uint32_t idesc;
+    int32_t act, bias_type;
+};
+
+struct LinearShared {
+    uint64_t full[LN_MAX_STAGES];
+    uint64_t empty[LN_MAX_STAGES];
+    uint64_t tmem_full[2];
+    uint64_t tmem_empty[2];
+    uint64_t drain;
+    uint32_t tmem_base;
+    int abort_flag;
+};
+
+__device__ __forceinline__ float load_as_float(const void *p, int64_t i, int type)
+{
+    if (type == CAT_F32) return reinterpret_cast<const float *>(p)[i];
+    if (type == CAT_BF16) return __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(p)[i]);
+    return __half2float(reinterpret_cast<const __half *>(p)[i]);
+}
+template <int T>
+struct Elem;
+template <>
+struct Elem<CAT_F32> {
+    using type = float;
+    static __device__ __forceinline__ float up(float v) { return v; }
+    static __device__ __forceinline__ float down(float v) { return v; }
+};
+template <>
+struct Elem<CAT_BF16> {
+    using type = __nv_bfloat16;
+    static __device__ __forceinline__ float up(__nv_bfloat16 v) { return __bfloat162float(v); }
+    static __device__ __forceinline__ __nv_bfloat16 down(float v) { return __float2bfloat16_rn(v); }
+};
+template <>
+struct Elem<CAT_F16> {
+    using type = __half;
+    static __device__ __forceinline__ float up(__half v) { return __half2float(v); }
+    static __device__ __forceinline__ __half down(float v) { return __float2half_rn(v); }
+};
+
+// gelu through erfc, which keeps its relative accuracy where 1 + erf(z) cancels; silu and gelu_tanh as z / (1 + e^-x): the tanh form
+// 0.5 z (1 + tanh u) is z / (1 + e^-2u).
+template <int ACT>
+__device__ __forceinline__ float activate(float z)
+{
+    if (ACT == CAT_ACT_RELU) return z < 0.f ? 0.f : z;   // (a NaN stays one)
+    if (ACT == CAT_ACT_GELU) return 0.5f * z * erfcf(-0.70710678f * z);
+    if (ACT == CAT_ACT_GELU_TANH) {
+        const float u = 0.7978845608f * z * fmaf(0.044715f * z, z, 1.f);
+        return z / (1.f + expf(-2.f * u));
+    }
+    if (ACT == CAT_ACT_SILU) return z / (1.f + expf(-z));
+    return z;
+}
+
+// 16 tokens of this thread's output column: y = act(acc + b) + r.  `count` tokens are there.
+template <int OT, int ACT>
+__device__ __forceinline__ void finish16(const float *acc, float bias, const typename Elem<OT>::type *res, int64_t ldr,
+                                         typename Elem<OT>::type *out, int64_t ldy, int count)
+{
+    using E = Elem<OT>;
+    typename E::type r[16];
+    if (res) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (j < count) r[j] = res[j * ldr];
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        float y = activate<ACT>(acc[j] + bias);
+        if (j < count) {
+            if (res) y += E::up(r[j]);
+            out[j * ldy] = E::down(y);
+        }
+    }
+}
+
+template <int OT>
+__device__ __forceinline__ void finish(int act, const float *acc, float bias, const typename Elem<OT>::type *res, int64_t ldr,
+                                       typename Elem<OT>::type *out, int64_t ldy, int count)
+{
+    switch (act) {
+    case CAT_ACT_RELU: finish16<OT, CAT_ACT_RELU>(acc, bias, res, ldr, out, ldy, count); break;
+    case CAT_ACT_GELU: finish16<OT, CAT_ACT_GELU>(acc, bias, res, ldr, out, ldy, count); break;
+    case CAT_ACT_GELU_TANH: finish16<OT, CAT_ACT_GELU_TANH>(acc, bias, res, ldr, out, ldy, count); break;
+    case CAT_ACT_SILU: finish16<OT, CAT_ACT_SILU>(acc, bias, res, ldr, out, ldy, count); break;
+    default: finish16<OT, CAT_ACT_NONE>(acc, bias, res, ldr, out, ldy, count); break;
+    }
+}
+
+__device__ __forceinline__ float activate_any(int act, float z)
+{
+    switch (act) {
+    case CAT_ACT_RELU: return activate<CAT_ACT_RELU>(z);
+    case CAT_ACT_GELU: return activate<CAT_ACT_GELU>(z);
+    case CAT_ACT_GELU_TANH: return activate<CAT_ACT_GELU_TANH>(z);
+    case CAT_ACT_SILU: return activate<CAT_ACT_SILU>(z);
+    default: return z;
+    }
+}
+
+__device__ __forceinline__ float ld_cluster_f32(uint32_t addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+// Unit -> tile.  LN_GROUP token tiles at a time sweep the weights, the tokens running fastest: the tiles in flight at a time are then
+// about as many of either operand, and what they read comes out of L2.
+__device__ __forceinline__ void tile_of(const LinearParams &p, int unit, int &tw, int &tt)
+{
+    const int full = LN_GROUP * p.tiles_w;
+    const int g = unit / full, rem = unit - g * full;
+    const int gs = min(LN_GROUP, p.tiles_t - g * LN_GROUP);
+    tw = rem / gs;
+    tt = g * LN_GROUP + rem - tw * gs;
+}
+
+template <bool PAIR, int OT>
+__global__ void __launch_bounds__(LN_THREADS, 1)
+linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapX, const __grid_constant__ LinearParams p)
+{
+    extern __shared__ unsigned char smem_raw[];
+    // (operand tiles start on 1024 bytes, as the swizzle wants)
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t ring = (raw + 1023u) & ~1023u;
+    unsigned char *ring_ptr = smem_raw + (ring - raw);
+    const int x_bytes = p.nt_cta * TC_SLAB_BYTES;
+    const int stage_bytes = TC_A_BYTES + x_bytes;
+    LinearShared &sh = *reinterpret_cast<LinearShared *>(ring_ptr + (size_t)p.stages * stage_bytes);
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t crank = (PAIR || p.splits > 1) ? cluster_ctarank() : 0u;
+    const uint32_t rank = PAIR ? crank : 0u;              // 0 = the CTA that issues the MMAs
+    const uint32_t split = PAIR ? 0u : crank;             // part of the inner dimension
+    volatile int *abort_flag = &sh.abort_flag;
+    constexpr int TW = PAIR ? 256 : 128;                  // output columns per tile
+    const int units = p.tiles_w * p.tiles_t;
+    const int per_cluster = PAIR ? 2 : p.splits;
+    const int unit_first = blockIdx.x / per_cluster, unit_step = gridDim.x / per_cluster;
+    const int slabs = (p.K + LN_BK - 1) / LN_BK;
+    const int slab0 = (int)((int64_t)slabs * split / p.splits), slab1 = (int)((int64_t)slabs * (split + 1) / p.splits);
+
+    if (tid == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            mbar_init(smem_u32(&sh.full[s]), PAIR ? 2 : 1);   // one expect_tx arrival per CTA
+            mbar_init(smem_u32(&sh.empty[s]), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(smem_u32(&sh.tmem_full[b]), 1);
+            mbar_init(smem_u32(&sh.tmem_empty[b]), (PAIR ? 2 : 1) * LN_EPI_WARPS);
+        }
+        mbar_init(smem_u32(&sh.drain), 1);
+        sh.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    pdl_enter();   // (before the TMEM allocation: the previous kernel of the stream has given its own back by then)
+    if (blockIdx.x == 0 && tid == 0) p.ctl->device_status = CAT_OK;   // (a wait that gives up does so seconds later)
+    if (warp == 1) {
+        if (PAIR) {
+            tmem_alloc_pair(smem_u32(&sh.tmem_base), (uint32_t)p.tmem_cols);
+            tmem_relinquish_pair();
+        } else {
+            tmem_alloc(smem_u32(&sh.tmem_base), (uint32_t)p.tmem_cols);
+            tmem_relinquish();
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync();   // the peer's barriers exist before anything arrives on them
+    tc_fence_after();
+    const uint32_t tmem_base = sh.tmem_base;
+
+    if (warp == 0) {
+        // ---------------------------------------------------------------- TMA producer of both operands
+        if (lane == 0) {
+            int s = 0;
+            uint32_t ph = 0;
+            bool ok = true;
+            for (int unit = unit_first; unit < units && ok; unit += unit_step) {
+                int tw, tt;
+                tile_of(p, unit, tw, tt);
+                const int n0 = tw * TW + (int)rank * 128;
+                const int t0 = tt * p.nt + (int)rank * p.nt_cta;
+                for (int sl = slab0; sl < slab1; ++sl) {
+                    if (!mbar_wait(smem_u32(&sh.empty[s]), ph ^ 1u, abort_flag, p.ctl)) { ok = false; break; }
+                    const uint32_t dst = ring + (uint32_t)(s * stage_bytes);
+                    if (PAIR) {
+                        const uint32_t full = mapa_cluster(smem_u32(&sh.full[s]), 0);
+                        mbar_arrive_expect_tx_cluster(full, (uint32_t)stage_bytes);
+                        tma_load_2d_pair(dst, &mapW, full, sl * LN_BK, n0);
+                        tma_load_2d_pair(dst + TC_A_BYTES, &mapX, full, sl * LN_BK, t0);
+                    } else {
+                        const uint32_t full = smem_u32(&sh.full[s]);
+                        mbar_arrive_expect_tx(full, (uint32_t)stage_bytes);
+                        tma_load_2d(dst, &mapW, full, sl * LN_BK, n0);
+                        tma_load_2d(dst + TC_A_BYTES, &mapX, full, sl * LN_BK, t0);
+                    }
+                    if (++s == p.stages) { s = 0; ph ^= 1u; }
+                }
+            }
+            if (!ok && rank == 0) {
+                // give copies that are still in flight a bounded time to land
+                for (int i = 0; i < p.stages; ++i)
+                    for (int tries = 0; tries < 100000; ++tries)
+                        if (mbar_try_wait(smem_u32(&sh.full[i]), 0) || mbar_try_wait(smem_u32(&sh.full[i]), 1)) break;
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------------------------------------------------------- MMA issuer
+        if (lane == 0 && rank == 0) {
+            const uint64_t wdesc0 = make_smem_desc(ring), xdesc0 = make_smem_desc(ring + TC_A_BYTES);
+            int s = 0;
+            uint32_t ph = 0, ti = 0;
+            bool ok = true;
+            for (int unit = unit_first; unit < units && ok; unit += unit_step, ++ti) {
+                const int b = ti & 1;
+                if (!mbar_wait(smem_u32(&sh.tmem_empty[b]), ((ti >> 1) & 1u) ^ 1u, abort_flag, p.ctl)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t acc = tmem_base + (uint32_t)(b * p.nt);
+                for (int sl = slab0; sl < slab1; ++sl) {
+                    if (!mbar_wait(smem_u32(&sh.full[s]), ph, abort_flag, p.ctl)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint64_t at = (uint64_t)(uint32_t)(s * (stage_bytes >> 4));
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk) {   // 16 inner columns = 32 B per MMA: +2 in 16-byte units
+                        const uint32_t accum = (sl > slab0 || kk > 0) ? 1u : 0u;
+                        if (PAIR) mma_f16_pair(acc, wdesc0 + at + 2 * kk, xdesc0 + at + 2 * kk, p.idesc, accum);
+                        else mma_f16(acc, wdesc0 + at + 2 * kk, xdesc0 + at + 2 * kk, p.idesc, accum);
+                    }
+                    if (PAIR) tc_commit_pair(smem_u32(&sh.empty[s]));
+                    else tc_commit(smem_u32(&sh.empty[s]));
+                    if (++s == p.stages) { s = 0; ph ^= 1u; }
+                }
+                if (ok) {
+                    if (PAIR) tc_commit_pair(smem_u32(&sh.tmem_full[b]));
+                    else tc_commit(smem_u32(&sh.tmem_full[b]));
+                }
+            }
+            // all MMAs issued by this thread have completed once this commit arrives
+            if (PAIR) tc_commit_pair_local(smem_u32(&sh.drain));
+            else tc_commit(smem_u32(&sh.drain));
+            for (int tries = 0; tries < 4000000; ++tries)
+                if (mbar_try_wait(smem_u32(&sh.drain), 0)) break;
+        }
+    } else {
+        // ---------------------------------------------------------------- epilogue
+        using E = Elem<OT>;
+        using T = typename E::type;
+        const int quarter = warp & 3, half = (warp - 2) >> 2;   // TMEM lanes this warp may read; which 16-column chunks it takes
+        uint32_t ti = 0;
+        for (int unit = unit_first; unit < units; unit += unit_step, ++ti) {
+            int tw, tt;
+            tile_of(p, unit, tw, tt);
+            const int b = ti & 1;
+            const int n = tw * TW + (int)rank * 128 + quarter * 32 + lane;
+            const bool inside = n < p.N;
+            const int64_t t0 = (int64_t)tt * p.nt;
+            const float bias = p.bias && inside && p.splits == 1 ? load_as_float(p.bias, n, p.bias_type) : 0.f;
+            if (!mbar_wait_warp(smem_u32(&sh.tmem_full[b]), (ti >> 1) & 1u, abort_flag, p.ctl)) break;
+            tc_fence_after();
+            const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * p.nt);
+            for (int c = half * 16; c < p.nt; c += 32) {
+                uint32_t raw16[16];
+                tmem_ld16_issue(taddr + (uint32_t)c, raw16);
+                tmem_ld_wait16(raw16);
+                float acc[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[j] = __uint_as_float(raw16[j]);
+                if (p.splits > 1) {
+                    // [token][output column] of this CTA's part, in the ring (every slab has been consumed)
+                    float *part = reinterpret_cast<float *>(ring_ptr) + (size_t)c * 128 + quarter * 32 + lane;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) part[j * 128] = acc[j];
+                } else if (inside && t0 + c < p.M) {
+                    const int64_t row = t0 + c;
+                    const int count = (int)min((int64_t)16, p.M - row);
+                    const T *res = p.residual ? reinterpret_cast<const T *>(p.residual) + row * p.ldr + n : nullptr;
+                    finish<OT>(p.act, acc, bias, res, p.ldr, reinterpret_cast<T *>(p.Y) + row * p.ldy + n, p.ldy, count);
+                }
+            }
+            // accumulator buffer b may be overwritten from here on
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (PAIR) mbar_arrive_cluster(mapa_cluster(smem_u32(&sh.tmem_empty[b]), 0));
+                else mbar_arrive(smem_u32(&sh.tmem_empty[b]));
+            }
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (!PAIR && p.splits > 1) {
+        // the parts meet: CTA r of the cluster adds every r-th run of 32 output columns, parts in order
+        using E = Elem<OT>;
+        using T = typename E::type;
+        cluster_sync();
+        int tw, tt;
+        tile_of(p, unit_first, tw, tt);
+        const int64_t t0 = (int64_t)tt * p.nt;
+        const int tokens = (int)min((int64_t)p.nt, p.M - t0);
+        const uint32_t part = ring;
+        if (*abort_flag == 0)
+            for (int g = (int)split + p.splits * warp; g < tokens * 4; g += p.splits * (LN_THREADS / 32)) {
+                const int t = g >> 2, n = tw * TW + (g & 3) * 32 + lane;
+                float v = 0.f;
+                for (int q = 0; q < p.splits; ++q)
+                    v += ld_cluster_f32(mapa_cluster(part + (uint32_t)((t * 128 + (g & 3) * 32 + lane) * 4), (uint32_t)q));
+                if (n < p.N) {
+                    const int64_t row = t0 + t;
+                    if (p.bias) v += load_as_float(p.bias, n, p.bias_type);
+                    v = activate_any(p.act, v);
+                    if (p.residual) v += E::up(reinterpret_cast<const T *>(p.residual)[row * p.ldr + n]);
+                    reinterpret_cast<T *>(p.Y)[row * p.ldy + n] = E::down(v);
+                }
+            }
+    }
+    if (PAIR || p.splits > 1) cluster_sync();   // no CTA's shared memory or TMEM goes away under another
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        if (PAIR) tmem_dealloc_pair(tmem_base, (uint32_t)p.tmem_cols);
+        else tmem_dealloc(tmem_base, (uint32_t)p.tmem_cols);
+    }
+}
+
+// Rows that TMA cannot address, copied to rows of `pitch` elements (zeros behind column K): 16-bit loads and stores of neighbouring lanes.
+__global__ void __launch_bounds__(256) linear_pad_kernel(const uint16_t *src, int64_t ld, int64_t rows, int K, int pitch, uint16_t *dst)
+{
+    pdl_enter();
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+        for (int k = threadIdx.x; k < pitch; k += blockDim.x) dst[r * pitch + k] = k < K ? src[r * ld + k] : (uint16_t)0;
+}
+
+bool tma_rows(const void *base, int64_t ld) { return (reinterpret_cast<uintptr_t>(base) & 15u) == 0 && ld % 8 == 0; }
+int padded(int K) { return (K + 7) & ~7; }
+
+struct LinearPlan {
+    bool pair;
+    int nt, splits;
+};
+
+LinearPlan plan(int64_t M, int N, int K, int sms)
+{
+    LinearPlan best{};
+    const int slabs = (K + LN_BK - 1) / LN_BK;
+    if (M > 128) {
+        best.pair = true;
+        best.splits = 1;
+        best.nt = (int)(M < 256 ? (M + 31) / 32 * 32 : 256);
+        return best;
+    }
+    best.nt = (int)((M + 15) / 16 * 16);
+    best.splits = 1;
+    const int tiles = (N + 127) / 128;
+    while (best.splits < 8 && tiles * best.splits * 2 <= sms && slabs >= best.splits * 4) best.splits *= 2;
+    return best;
+}
+
+}  // namespace
+
+size_t linear_workspace_bytes(const void *X, int64_t ldx, const void *W, int64_t ldw, int64_t M, int N, int K)
+{
+    size_t n = 256;
+    if (!tma_rows(X, ldx)) n += align_up((size_t)M * padded(K) * 2, 256);
+    if (!tma_rows(W, ldw)) n += align_up((size_t)N * padded(K) * 2, 256);
+    return n;
+}
+
+cudaError_t launch_linear(const LinearArgs &a, void *workspace, cudaStream_t s)
+{
+    const int sms = tc_sm_count();
+    unsigned char *room = reinterpret_cast<unsigned char *>(workspace) + 256;
+    const void *X = a.X, *W = a.W;
+    int64_t ldx = a.ldx, ldw = a.ldw;
+    cudaError_t e;
+    auto pad = [&](const void *&src, int64_t &ld, int64_t rows) {
+        const int64_t blocks = rows < 16 * sms ? rows : 16 * sms;
+        const cudaError_t r = launch_pdl(linear_pad_kernel, dim3((unsigned)blocks), dim3(256), 0, s, reinterpret_cast<const uint16_t *>(src), ld,
+                                         rows, a.K, padded(a.K), reinterpret_cast<uint16_t *>(room));
+        count_launch();
+        src = room;
+        ld = padded(a.K);
+        room += align_up((size_t)rows * padded(a.K) * 2, 256);
+        return r;
+    };
+    if (!tma_rows(X, ldx) && (e = pad(X, ldx, a.M)) != cudaSuccess) return e;
+    if (!tma_rows(W, ldw) && (e = pad(W, ldw, a.N)) != cudaSuccess) return e;
+
+    const LinearPlan pl = plan(a.M, a.N, a.K, sms);
+    LinearParams p{};
+    p.bias = a.bias;
+    p.residual = a.residual;
+    p.Y = a.Y;
+    p.ctl = reinterpret_cast<Control *>(workspace);
+    p.ldr = a.ldr;
+    p.ldy = a.ldy;
+    p.M = a.M;
+    p.N = a.N;
+    p.K = a.K;
+    p.nt = pl.nt;
+    p.nt_cta = pl.pair ? pl.nt / 2 : pl.nt;
+    p.tiles_w = (a.N + (pl.pair ? 255 : 127)) / (pl.pair ? 256 : 128);
+    p.tiles_t = (int)((a.M + pl.nt - 1) / pl.nt);
+    p.splits = pl.splits;
+    p.act = a.act;
+    p.bias_type = a.bias_type;
+    int cols = 32;
+    while (cols < 2 * pl.nt) cols <<= 1;
+    p.tmem_cols = cols;
+    p.idesc = make_idesc(pl.pair ? 256 : 128, pl.nt, a.in_type == CAT_BF16 ? 1u : 0u);
+
+    CUtensorMap mapW, mapX;
+    if (!tc_make_map16(&mapW, W, a.in_type == CAT_BF16, a.N, a.K, ldw, TC_BM) ||
+        !tc_make_map16(&mapX, X, a.in_type == CAT_BF16, a.M, a.K, ldx, p.nt_cta))
+        return cudaErrorInvalidValue;
+
+    const int stage_bytes = TC_A_BYTES + p.nt_cta * TC_SLAB_BYTES;
+    const int64_t units = (int64_t)p.tiles_w * p.tiles_t;
+    const int room_smem = 227 * 1024 - 1024 - (int)sizeof(LinearShared);
+    p.stages = room_smem / stage_bytes;
+    if (p.stages > LN_MAX_STAGES) p.stages = LN_MAX_STAGES;
+    const size_t smem = 1024 + (size_t)p.stages * stage_bytes + sizeof(LinearShared);
+    const int per_cluster = pl.pair ? 2 : pl.splits;
+    int64_t clusters = sms / per_cluster;
+    if (units < clusters) clusters = units;
+    if (pl.splits > 1 && clusters < units) return cudaErrorInvalidValue;   // (a split tile is a cluster's only one)
+
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(clusters * per_cluster), 1, 1);
+    cfg.blockDim = dim3(LN_THREADS, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)per_cluster;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // (the kernel calls pdl_enter)
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+
+#define CAT_LINEAR_LAUNCH(PAIR, OT)                                                                                             \
+    do {                                                                                                                        \
+        auto kern = linear_kernel<PAIR, OT>;                                                                                    \
+        if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024)) != cudaSuccess) return e; \
+        e = cudaLaunchKernelEx(&cfg, kern, mapW, mapX, p);                                                                      \
+    } while (0)
+    if (pl.pair) {
+        if (a.out_type == CAT_F32) CAT_LINEAR_LAUNCH(true, CAT_F32);
+        else if (a.out_type == CAT_BF16) CAT_LINEAR_LAUNCH(true, CAT_BF16);
+        else CAT_LINEAR_LAUNCH(true, CAT_F16);
+    } else {
+        if (a.out_type == CAT_F32) CAT_LINEAR_LAUNCH(false, CAT_F32);
+        else if (a.out_type == CAT_BF16) CAT_LINEAR_LAUNCH(false, CAT_BF16);
+        else CAT_LINEAR_LAUNCH(false, CAT_F16);
+    }
+#undef CAT_LINEAR_LAUNCH
+    count_launch();
+    return e;
+}
+
+}  // namespace cat

@@ -1302,22 +1302,27 @@ EncodeTiledFn encode_fn()
     return fn;
 }
 
-// 2-D row-major [rows, D] of fp32 (or fp16: rows half_ld(D) apart) viewed in boxes of box_rows x 128
+// 2-D row-major [rows, D] of a type of esz bytes, rows ld elements apart, viewed in boxes of box_rows x 128
 // bytes, 128-byte swizzle, zero fill outside the matrix.
-bool make_map(CUtensorMap *map, const void *base, bool half, int64_t rows, int D, int box_rows)
+bool encode_map(CUtensorMap *map, const void *base, CUtensorMapDataType type, size_t esz, int64_t rows, int D, int64_t ld, int box_rows)
 {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
-    const size_t esz = half ? 2 : 4;
     cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)rows};
-    cuuint64_t strides[1] = {(cuuint64_t)(half ? half_ld(D) : D) * esz};
+    cuuint64_t strides[1] = {(cuuint64_t)ld * esz};
     cuuint32_t box[2] = {(cuuint32_t)(TC_SLAB_BYTES / esz), (cuuint32_t)box_rows};
     cuuint32_t estr[2] = {1, 1};
-    CUresult r = fn(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2,
-                    const_cast<void *>(base), dims, strides, box, estr,
+    CUresult r = fn(map, type, 2, const_cast<void *>(base), dims, strides, box, estr,
                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS;
+}
+
+// A matrix of fp32, or its fp16 copy (rows half_ld(D) apart).
+bool make_map(CUtensorMap *map, const void *base, bool half, int64_t rows, int D, int box_rows)
+{
+    return half ? encode_map(map, base, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, rows, D, half_ld(D), box_rows)
+                : encode_map(map, base, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, rows, D, D, box_rows);
 }
 
 // The affine kernel re-divides its registers among its warpgroups; a division larger than
@@ -1354,6 +1359,11 @@ int sm_count()
 bool tc_make_map(CUtensorMap *map, const void *base, bool half, int64_t rows, int D, int box_rows)
 {
     return make_map(map, base, half, rows, D, box_rows);
+}
+
+bool tc_make_map16(CUtensorMap *map, const void *base, bool bf16, int64_t rows, int D, int64_t ld, int box_rows)
+{
+    return encode_map(map, base, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, rows, D, ld, box_rows);
 }
 
 int tc_sm_count() { return sm_count(); }

@@ -17,6 +17,8 @@ namespace cat {
 // A 2-D row-major [rows, D] matrix of fp32 (or fp16) viewed in boxes of box_rows x 128 bytes with
 // the 128-byte swizzle and zero fill outside the matrix; false if the encoder is unavailable.
 bool tc_make_map(CUtensorMap *map, const void *base, bool half, int64_t rows, int D, int box_rows);
+// The same for a matrix of bf16 or fp16 whose rows are ld elements apart (a multiple of 8).
+bool tc_make_map16(CUtensorMap *map, const void *base, bool bf16, int64_t rows, int D, int64_t ld, int box_rows);
 int tc_sm_count();
 
 namespace {
