@@ -382,6 +382,39 @@ cat_status_t cat_linear(const void *X, int64_t ldx, const void *W, int64_t ldw, 
                         const void *residual, int64_t ldr, int32_t activation, int64_t M, int32_t N, int32_t K,
                         void *Y, int64_t ldy, int32_t out_type, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Verification of drafted tokens: the low-bit network (its logits corrected by cat_apply or not) has drafted up to S tokens
+ * for each of B sequences, the full-precision one has computed its logits behind each of them in one pass; this call says
+ * how many drafts stand and draws the token that follows them, such that the tokens are distributed as if the target had drawn
+ * them one by one.  A sequence without drafts is plain sampling from its row (which is how drafts are drawn).
+ *   p_j = softmax(target[b,j,:] / T_b), q_j = softmax(draft[b,j,:] / T_b)
+ *   draft j is accepted iff  u_accept[b,j] q_j(x_j) < p_j(x_j);  the first one that is not ends the sequence, and the next
+ *   token is drawn from max(p_j - q_j, 0);  if all are accepted it is drawn from the row behind the last.
+ *   A draw is the first index at which the cumulated mass exceeds u_sample[b] times the whole mass.
+ * target [B, S+1, V] and draft [B, S, V] of any of the three types each; rows target_row / draft_row elements apart (at least V),
+ * sequences target_seq / draft_seq apart; no alignment beyond the element's.  draft = NULL: the drafts were not sampled (from a
+ * lookup, say): q_j is 1 at x_j.  draft_tokens [B, S] int32; a token outside [0, V) is refused.  draft_lengths [B], may be NULL (S
+ * each): how many of its S places a sequence uses (more than S counts as S); a sequence of length < 0 is not there, and its outputs are left as they
+ * were.  Entries behind a sequence's length are not looked at.  temperature [B], may be NULL (1 each): T <= 0 is greedy decoding --
+ * all mass on the row's largest entry, the lowest index of equal ones; NaN counts as 0.  u_accept [B, S], u_sample [B]: uniform
+ * numbers in [0, 1), given, so that a call is reproducible (others are brought into [0, 1 - 2^-24], NaN counts as 0).
+ * tokens_out [B, S+1]: the accepted drafts, the drawn token, -1 behind it.  accepted_out [B]: how many were accepted.
+ * Logits: -inf (a mask) and NaN have no mass, +inf counts as the largest finite number.  A row without any mass accepts
+ * nothing and gives token -1.  A residual of less mass than 2^-40 is what rounding left of none: the draw is from p_j then.
+ * The outputs are those of fp64 arithmetic: what fast fp32 sums cannot decide within their error bound goes to an fp64 pass
+ * (cat_workspace_report counts those sequences).  S = 0 is allowed (draft, draft_tokens and u_accept may be NULL then), B = 0 does nothing.
+ * Limits: B <= CAT_VERIFY_MAX_B, S <= CAT_VERIFY_MAX_S, V <= CAT_VERIFY_MAX_V.  Workspace: CAT_VERIFY_WORKSPACE_BYTES.
+ */
+#define CAT_VERIFY_MAX_B (1 << 20)
+#define CAT_VERIFY_MAX_S 256
+#define CAT_VERIFY_MAX_V (1 << 22)
+#define CAT_VERIFY_WORKSPACE_BYTES 256
+cat_status_t cat_verify_drafts(const void *target, int32_t target_type, int64_t target_seq, int64_t target_row,
+                               const void *draft, int32_t draft_type, int64_t draft_seq, int64_t draft_row,
+                               const int32_t *draft_tokens, const int32_t *draft_lengths, const float *temperature,
+                               const float *u_accept, const float *u_sample, int32_t B, int32_t S, int32_t V,
+                               int32_t *tokens_out, int32_t *accepted_out, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- host-buffer entry points (end-to-end use) ------------------------- */
 
 /*

@@ -38,7 +38,7 @@ EXPORTS = [
     "cat_fit_shard_begin", "cat_fit_shard_round", "cat_fit_shard_update",
     "cat_pca_workspace_bytes", "cat_pca_fit", "cat_pca_project", "cat_affine_with_labels",
     "cat_fit_pca_workspace_bytes", "cat_fit_pca", "cat_apply_pca_workspace_bytes", "cat_apply_pca",
-    "cat_linear_workspace_bytes", "cat_linear",
+    "cat_linear_workspace_bytes", "cat_linear", "cat_verify_drafts",
     "cat_centroids_from_sums",
     "cat_centred_moments", "cat_solve_gamma_beta", "cat_apply_host_workspace_bytes",
     "cat_apply_host", "cat_fit_host_workspace_bytes", "cat_fit_host", "cat_workspace_report",
@@ -132,6 +132,8 @@ def lib():
     L.cat_linear_workspace_bytes.restype = sz
     L.cat_linear.argtypes = [vp, i64, vp, i64, i32, vp, i32, vp, i64, i32, i64, i32, i32, vp, i64, i32, vp, sz, vp]
     L.cat_linear.restype = ctypes.c_int
+    L.cat_verify_drafts.argtypes = [vp, i32, i64, i64, vp, i32, i64, i64, vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, sz, vp]
+    L.cat_verify_drafts.restype = ctypes.c_int
     L.cat_selftest_wait_timeout.argtypes = [vp, sz, i32, vp]
     L.cat_selftest_wait_timeout.restype = ctypes.c_int
     L.cat_workspace_report.argtypes = [vp, vp, vp, vp, vp]
@@ -602,6 +604,64 @@ def cat_linear(X, W, bias=None, residual=None, activation: str = "none", out=Non
 
     _check(_call_on(device, call), "cat_linear")
     return out
+
+
+def _vector(t: Optional[torch.Tensor], dtype, shape, name: str, device: torch.device):
+    if t is None:
+        return None
+    if t.device != device or t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype} on {device}, got {t.dtype} on {t.device}")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous of shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _rows(t: torch.Tensor, shape, name: str, device: torch.device):
+    """(address, type, distance of sequences, distance of rows) of [sequences, rows, V] logits with contiguous rows."""
+    if t.device != device or t.dtype not in _TYPES:
+        raise TypeError(f"{name} must be fp32, bf16 or fp16 on {device}, got {t.dtype} on {t.device}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    seq, row, step = t.stride()
+    if step != 1 and shape[2] > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return t.data_ptr(), _TYPES[t.dtype], seq, row
+
+
+def cat_verify_drafts(target, draft, draft_tokens, u_accept, u_sample, draft_lengths=None, temperature=None, tokens_out=None,
+                      accepted_out=None, ws=None):
+    """cat_verify_drafts: (tokens [B, S + 1] int32, accepted [B] int32) for target [B, S + 1, V] and draft [B, S, V] logits (None:
+    drafts without probabilities), draft_tokens [B, S] int32, uniform numbers u_accept [B, S] and u_sample [B] fp32, lengths [B]
+    int32 and temperatures [B] fp32 (see cat.h)."""
+    device = target.device
+    if device.type != "cuda":
+        raise TypeError("target must be a CUDA tensor")
+    if target.dim() != 3:
+        raise ValueError("target must have shape [B, S + 1, V]")
+    B, S, V = target.shape
+    S -= 1
+    if S < 0:
+        raise ValueError("target must have a row behind the drafts")
+    t = _rows(target, target.shape, "target", device)
+    q = (None, 0, 0, 0) if draft is None else _rows(draft, (B, S, V), "draft", device)
+    vectors = (_vector(draft_tokens, torch.int32, (B, S), "draft_tokens", device),
+               _vector(draft_lengths, torch.int32, (B,), "draft_lengths", device),
+               _vector(temperature, torch.float32, (B,), "temperature", device),
+               _vector(u_accept, torch.float32, (B, S), "u_accept", device), _vector(u_sample, torch.float32, (B,), "u_sample", device))
+    if tokens_out is None:
+        tokens_out = torch.empty((B, S + 1), dtype=torch.int32, device=device)
+    if accepted_out is None:
+        accepted_out = torch.empty((B,), dtype=torch.int32, device=device)
+    outs = (_vector(tokens_out, torch.int32, (B, S + 1), "tokens_out", device),
+            _vector(accepted_out, torch.int32, (B,), "accepted_out", device))
+    L = lib()
+
+    def call(stream):
+        room = _control_block(device, stream) if ws is None else ws
+        return L.cat_verify_drafts(*t, *q, *vectors, B, S, V, *outs, room.data_ptr(), room.numel() * room.element_size(), stream)
+
+    _check(_call_on(device, call), "cat_verify_drafts")
+    return tokens_out, accepted_out
 
 
 def cat_apply_host(Yq_host, centroids_host, gamma_host, beta_host, out_host, labels_host=None,

@@ -876,6 +876,30 @@ cat_status_t cat_linear(const void *X, int64_t ldx, const void *W, int64_t ldw, 
     return CAT_OK;
 }
 
+cat_status_t cat_verify_drafts(const void *target, int32_t target_type, int64_t target_seq, int64_t target_row,
+                               const void *draft, int32_t draft_type, int64_t draft_seq, int64_t draft_row,
+                               const int32_t *draft_tokens, const int32_t *draft_lengths, const float *temperature,
+                               const float *u_accept, const float *u_sample, int32_t B, int32_t S, int32_t V,
+                               int32_t *tokens_out, int32_t *accepted_out, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (B < 0 || S < 0 || V < 1 || !is_type(target_type) || (draft && !is_type(draft_type))) return CAT_ERR_SHAPE;
+    if (B > CAT_VERIFY_MAX_B || S > CAT_VERIFY_MAX_S || V > CAT_VERIFY_MAX_V) return CAT_ERR_UNSUPPORTED;
+    // (a distance says nothing where there is one row, or one sequence)
+    if ((S > 0 && target_row < V) || (S > 1 && draft && draft_row < V)) return CAT_ERR_SHAPE;
+    if (B > 1 && (target_seq < V || (S > 0 && draft && draft_seq < V))) return CAT_ERR_SHAPE;
+    if (B == 0) return CAT_OK;
+    if (!target || !u_sample || !tokens_out || !accepted_out || (S > 0 && (!draft_tokens || !u_accept))) return CAT_ERR_NULL;
+    if (misaligned(target, target_type) || (draft && misaligned(draft, draft_type)) || misaligned(draft_tokens, CAT_F32) ||
+        misaligned(draft_lengths, CAT_F32) || misaligned(temperature, CAT_F32) || misaligned(u_accept, CAT_F32) || misaligned(u_sample, CAT_F32) ||
+        misaligned(tokens_out, CAT_F32) || misaligned(accepted_out, CAT_F32))
+        return CAT_ERR_ALIGN;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < CAT_VERIFY_WORKSPACE_BYTES) return CAT_ERR_WORKSPACE;
+    const VerifyArgs a{target, S > 0 ? draft : nullptr, draft_tokens, draft_lengths, temperature, u_accept, u_sample, tokens_out, accepted_out,
+                       target_seq, target_row, draft_seq, draft_row, target_type, draft_type, B, S, V};
+    CAT_CUDA(launch_verify(a, workspace, reinterpret_cast<cudaStream_t>(stream)));
+    return CAT_OK;
+}
+
 cat_status_t cat_workspace_report(const void *workspace, void *stream, int64_t *refined_last_host,
                                   int64_t *refined_total_host, int32_t *device_status_host)
 {

@@ -395,4 +395,15 @@ struct LinearArgs {
 size_t linear_workspace_bytes(const void *X, int64_t ldx, const void *W, int64_t ldw, int64_t M, int N, int K);
 cudaError_t launch_linear(const LinearArgs &a, void *workspace, cudaStream_t s);
 
+// Verification of drafted tokens (cat_verify.cu); fields as in cat.h.
+struct VerifyArgs {
+    const void *target, *draft;
+    const int32_t *tokens, *lengths;
+    const float *temperature, *u_accept, *u_sample;
+    int32_t *tokens_out, *accepted_out;
+    int64_t target_seq, target_row, draft_seq, draft_row;
+    int32_t target_type, draft_type, B, S, V;
+};
+cudaError_t launch_verify(const VerifyArgs &a, void *workspace, cudaStream_t s);
+
 }  // namespace cat
