@@ -403,6 +403,7 @@ cat_status_t cat_linear(const void *X, int64_t ldx, const void *W, int64_t ldw, 
  * nothing and gives token -1.  A residual of less mass than 2^-40 is what rounding left of none: the draw is from p_j then.
  * The outputs are those of fp64 arithmetic: what fast fp32 sums cannot decide within their error bound goes to an fp64 pass
  * (cat_workspace_report counts those sequences).  S = 0 is allowed (draft, draft_tokens and u_accept may be NULL then), B = 0 does nothing.
+ * The outputs overlap neither each other nor an input.
  * Limits: B <= CAT_VERIFY_MAX_B, S <= CAT_VERIFY_MAX_S, V <= CAT_VERIFY_MAX_V.  Workspace: CAT_VERIFY_WORKSPACE_BYTES.
  */
 #define CAT_VERIFY_MAX_B (1 << 20)

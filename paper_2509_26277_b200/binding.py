@@ -539,7 +539,7 @@ def _control_block(device: torch.device, stream: int) -> torch.Tensor:
     """The 256-byte workspace of the calls that need no more, one per stream (cat_workspace_report reads it)."""
     ws = _control_blocks.get((device.index, stream))
     if ws is None:
-        ws = _control_blocks[(device.index, stream)] = torch.empty(256, dtype=torch.uint8, device=device)
+        ws = _control_blocks[(device.index, stream)] = torch.zeros(256, dtype=torch.uint8, device=device)
     return ws
 
 

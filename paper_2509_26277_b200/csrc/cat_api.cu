@@ -838,6 +838,12 @@ cat_status_t cat_solve_gamma_beta(const double *sumQ, const double *sumF, const 
 static bool is_type(int32_t t) { return t == CAT_F32 || t == CAT_BF16 || t == CAT_F16; }
 static bool misaligned(const void *p, int32_t type) { return reinterpret_cast<uintptr_t>(p) & (type == CAT_F32 ? 3u : 1u); }
 
+static bool overlap(const void *a, size_t n, const void *b, size_t m)
+{
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+    return p && q && p < q + m && q < p + n;
+}
+
 // (the distance of the only row of a matrix says nothing)
 static int64_t row_distance(int64_t ld, int64_t rows, int32_t K) { return rows > 1 ? ld : ((int64_t)K + 7) & ~(int64_t)7; }
 
@@ -893,6 +899,14 @@ cat_status_t cat_verify_drafts(const void *target, int32_t target_type, int64_t 
         misaligned(draft_lengths, CAT_F32) || misaligned(temperature, CAT_F32) || misaligned(u_accept, CAT_F32) || misaligned(u_sample, CAT_F32) ||
         misaligned(tokens_out, CAT_F32) || misaligned(accepted_out, CAT_F32))
         return CAT_ERR_ALIGN;
+    // the CTAs that share a sequence read these again and again: an output among them would make them disagree
+    const size_t n = (size_t)B, s = (size_t)S;
+    const struct { const void *at; size_t bytes; } in[] = {{draft_tokens, 4 * n * s}, {draft_lengths, 4 * n}, {temperature, 4 * n}, {u_accept, 4 * n * s}, {u_sample, 4 * n}};
+    const struct { const void *at; size_t bytes; } out[] = {{tokens_out, 4 * n * (s + 1)}, {accepted_out, 4 * n}};
+    for (const auto &o : out)
+        for (const auto &i : in)
+            if (overlap(o.at, o.bytes, i.at, i.bytes)) return CAT_ERR_SHAPE;
+    if (overlap(out[0].at, out[0].bytes, out[1].at, out[1].bytes)) return CAT_ERR_SHAPE;
     if (!workspace || !aligned16(workspace) || workspace_bytes < CAT_VERIFY_WORKSPACE_BYTES) return CAT_ERR_WORKSPACE;
     const VerifyArgs a{target, S > 0 ? draft : nullptr, draft_tokens, draft_lengths, temperature, u_accept, u_sample, tokens_out, accepted_out,
                        target_seq, target_row, draft_seq, draft_row, target_type, draft_type, B, S, V};

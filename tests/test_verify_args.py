@@ -10,7 +10,7 @@ AT = 0x100000          # never dereferenced: every call below fails validation f
 
 def call(**over):
     a = dict(target=AT, tt=1, ts=500, tr=100, draft=AT, dt=0, ds=400, dr=100, tokens=AT, lengths=None, temperature=None, ua=AT, us=AT, B=2, S=4,
-             V=100, out=AT, kept=AT, ws=AT, ws_bytes=256)
+             V=100, out=AT + 4096, kept=AT + 8192, ws=AT, ws_bytes=256)
     a.update(over)
     return B.lib().cat_verify_drafts(a["target"], a["tt"], a["ts"], a["tr"], a["draft"], a["dt"], a["ds"], a["dr"], a["tokens"], a["lengths"],
                                      a["temperature"], a["ua"], a["us"], a["B"], a["S"], a["V"], a["out"], a["kept"], a["ws"], a["ws_bytes"], None)
@@ -21,7 +21,8 @@ BAD = [(dict(target=None), 1), (dict(us=None), 1), (dict(out=None), 1), (dict(ke
        (dict(ds=0), 2), (dict(B=(1 << 20) + 1), 7), (dict(S=257), 7), (dict(V=(1 << 22) + 1), 7),
        (dict(target=AT + 1), 3), (dict(draft=AT + 2), 3), (dict(tokens=AT + 2), 3), (dict(lengths=AT + 1), 3), (dict(temperature=AT + 2), 3),
        (dict(ua=AT + 1), 3), (dict(us=AT + 2), 3), (dict(out=AT + 2), 3), (dict(kept=AT + 3), 3),
-       (dict(ws=None), 4), (dict(ws_bytes=255), 4), (dict(ws=AT + 4), 4)]
+       (dict(tokens=AT + 4096 + 36), 2), (dict(ua=AT + 4064 + 4), 2), (dict(us=AT + 8196), 2), (dict(lengths=AT + 8192), 2), (dict(temperature=AT + 4096), 2),
+       (dict(kept=AT + 4096 + 36), 2), (dict(ws=None), 4), (dict(ws_bytes=255), 4), (dict(ws=AT + 4), 4)]
 
 
 @pytest.mark.parametrize("over,status", BAD)
