@@ -527,27 +527,25 @@ ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}      
 _control_blocks = {}
 
 
-def _call_on(device: torch.device, call):
-    """call(raw stream) with `device` current and its current stream (the library launches on the current device)."""
-    if device.index == torch.cuda.current_device():
-        return call(torch._C._cuda_getCurrentRawStream(device.index))
-    with torch.cuda.device(device):
-        return call(torch._C._cuda_getCurrentRawStream(device.index))
-
-
-def _control_block(device: torch.device, stream: int) -> torch.Tensor:
+def _control_block(index: int, stream: int) -> torch.Tensor:
     """The 256-byte workspace of the calls that need no more, one per stream (cat_workspace_report reads it)."""
-    ws = _control_blocks.get((device.index, stream))
+    ws = _control_blocks.get((index, stream))
     if ws is None:
-        ws = _control_blocks[(device.index, stream)] = torch.zeros(256, dtype=torch.uint8, device=device)
+        ws = _control_blocks[(index, stream)] = torch.zeros(256, dtype=torch.uint8, device=torch.device("cuda", index))
     return ws
+
+
+def _on_device(t: torch.Tensor, call, *args, **kwargs):
+    """The call again with t's device current (the library launches on the current device)."""
+    with torch.cuda.device(t.device):
+        return call(*args, **kwargs)
 
 
 def _matrix(t: torch.Tensor, name: str, device: torch.device, rows: int, cols: int) -> int:
     """Distance of the rows of a 2-D device matrix whose columns are contiguous."""
     if t.device != device:
         raise TypeError(f"{name} must be a CUDA tensor on {device}, not on {t.device}")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+    if t.shape != (rows, cols):
         raise ValueError(f"{name} must have shape {(rows, cols)}, got {tuple(t.shape)}")
     ld, step = t.stride()
     if step != 1 and cols > 1:
@@ -555,60 +553,69 @@ def _matrix(t: torch.Tensor, name: str, device: torch.device, rows: int, cols: i
     return ld
 
 
+# (These two are called for a token at a time: a call's checks and marshalling are kept short, about five microseconds.)
+
 def cat_linear(X, W, bias=None, residual=None, activation: str = "none", out=None, out_dtype=None, ws=None):
     """cat_linear: act(X W^T + bias) + residual for X [M, K] and W [N, K] in bf16 or fp16, [M, N] of out_dtype (default:
     X's; residual's and out's type has to be the same).  Rows may be any distance apart."""
-    device = X.device
-    if device.type != "cuda":
+    device, dtype = X.device, X.dtype
+    if not X.is_cuda:
         raise TypeError("X must be a CUDA tensor")
+    index = device.index
+    if index != torch._C._cuda_getDevice():
+        return _on_device(X, cat_linear, X, W, bias, residual, activation, out, out_dtype, ws)
     if X.dim() != 2 or W.dim() != 2:
         raise ValueError("X and W must be matrices")
     M, K = X.shape
     N = W.shape[0]
-    in_type = _TYPES.get(X.dtype, 0)
-    if in_type == 0 or W.dtype != X.dtype:
-        raise TypeError(f"X and W must both be bf16 or both fp16, got {X.dtype} and {W.dtype}")
-    if activation not in ACTIVATIONS:
+    in_type = _TYPES.get(dtype, 0)
+    if in_type == 0 or W.dtype != dtype:
+        raise TypeError(f"X and W must both be bf16 or both fp16, got {dtype} and {W.dtype}")
+    act = ACTIVATIONS.get(activation)
+    if act is None:
         raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")
     ldx, ldw = _matrix(X, "X", device, M, K), _matrix(W, "W", device, N, K)
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype or X.dtype, device=device)
-    elif out_dtype is not None and out.dtype != out_dtype:
-        raise TypeError(f"out must be {out_dtype}, got {out.dtype}")
-    if out.dtype not in _TYPES:
-        raise TypeError(f"out must be fp32, bf16 or fp16, got {out.dtype}")
-    ldy, ldr = _matrix(out, "out", device, M, N), 0
+        if out_dtype is None:
+            out_dtype = dtype
+        elif out_dtype not in _TYPES:
+            raise TypeError(f"out_dtype must be fp32, bf16 or fp16, got {out_dtype}")
+        ldy = N
+        out = torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=device)
+    else:
+        if out.dtype not in _TYPES or (out_dtype is not None and out.dtype != out_dtype):
+            raise TypeError(f"out must be {out_dtype or 'fp32, bf16 or fp16'}, got {out.dtype}")
+        out_dtype = out.dtype
+        ldy = _matrix(out, "out", device, M, N)
+    b = r = None
+    ldr = bias_type = 0
     if residual is not None:
         ldr = _matrix(residual, "residual", device, M, N)
-        if residual.dtype != out.dtype:
-            raise TypeError(f"residual must be {out.dtype} as the output is, got {residual.dtype}")
+        if residual.dtype != out_dtype:
+            raise TypeError(f"residual must be {out_dtype} as the output is, got {residual.dtype}")
+        r = residual.data_ptr()
     if bias is not None:
-        if bias.device != device or bias.dtype not in _TYPES:
+        bias_type = _TYPES.get(bias.dtype)
+        if bias.device != device or bias_type is None:
             raise TypeError(f"bias must be fp32, bf16 or fp16 on {device}")
         if bias.shape != (N,) or not bias.is_contiguous():
             raise ValueError(f"bias must be contiguous of shape {(N,)}")
-    L = lib()
-    x, w = X.data_ptr(), W.data_ptr()
-
-    def call(stream):
-        room = ws
-        if room is None:
-            if (x | w) & 15 or (M > 1 and ldx & 7) or (N > 1 and ldw & 7):   # (copies of rows that the kernel cannot address)
-                room = torch.empty(max(256, L.cat_linear_workspace_bytes(x, ldx, w, ldw, M, N, K)), dtype=torch.uint8, device=device)
-            else:
-                room = _control_block(device, stream)
-        return L.cat_linear(x, ldx, w, ldw, in_type, bias.data_ptr() if bias is not None else None,
-                            _TYPES[bias.dtype] if bias is not None else 0, residual.data_ptr() if residual is not None else None, ldr,
-                            ACTIVATIONS[activation], M, N, K, out.data_ptr(), ldy, _TYPES[out.dtype], room.data_ptr(),
-                            room.numel() * room.element_size(), stream)
-
-    _check(_call_on(device, call), "cat_linear")
+        b = bias.data_ptr()
+    L = _lib or lib()
+    x, w, stream = X.data_ptr(), W.data_ptr(), torch._C._cuda_getCurrentRawStream(index)
+    if ws is None:
+        if (x | w) & 15 or (M > 1 and ldx & 7) or (N > 1 and ldw & 7):   # (copies of rows that the kernel cannot address)
+            ws = torch.empty(max(256, L.cat_linear_workspace_bytes(x, ldx, w, ldw, M, N, K)), dtype=torch.uint8, device=device)
+        else:
+            ws = _control_block(index, stream)
+    st = L.cat_linear(x, ldx, w, ldw, in_type, b, bias_type, r, ldr, act, M, N, K, out.data_ptr(), ldy, _TYPES[out_dtype],
+                      ws.data_ptr(), ws.nbytes, stream)
+    if st != CAT_OK:
+        raise CatError(st, "cat_linear")
     return out
 
 
-def _vector(t: Optional[torch.Tensor], dtype, shape, name: str, device: torch.device):
-    if t is None:
-        return None
+def _vector(t: torch.Tensor, dtype, shape, name: str, device: torch.device) -> int:
     if t.device != device or t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype} on {device}, got {t.dtype} on {t.device}")
     if t.shape != shape or not t.is_contiguous():
@@ -618,14 +625,15 @@ def _vector(t: Optional[torch.Tensor], dtype, shape, name: str, device: torch.de
 
 def _rows(t: torch.Tensor, shape, name: str, device: torch.device):
     """(address, type, distance of sequences, distance of rows) of [sequences, rows, V] logits with contiguous rows."""
-    if t.device != device or t.dtype not in _TYPES:
+    kind = _TYPES.get(t.dtype)
+    if t.device != device or kind is None:
         raise TypeError(f"{name} must be fp32, bf16 or fp16 on {device}, got {t.dtype} on {t.device}")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     seq, row, step = t.stride()
     if step != 1 and shape[2] > 1:
         raise ValueError(f"{name} must have contiguous rows")
-    return t.data_ptr(), _TYPES[t.dtype], seq, row
+    return t.data_ptr(), kind, seq, row
 
 
 def cat_verify_drafts(target, draft, draft_tokens, u_accept, u_sample, draft_lengths=None, temperature=None, tokens_out=None,
@@ -634,33 +642,41 @@ def cat_verify_drafts(target, draft, draft_tokens, u_accept, u_sample, draft_len
     drafts without probabilities), draft_tokens [B, S] int32, uniform numbers u_accept [B, S] and u_sample [B] fp32, lengths [B]
     int32 and temperatures [B] fp32 (see cat.h)."""
     device = target.device
-    if device.type != "cuda":
+    if not target.is_cuda:
         raise TypeError("target must be a CUDA tensor")
+    index = device.index
+    if index != torch._C._cuda_getDevice():
+        return _on_device(target, cat_verify_drafts, target, draft, draft_tokens, u_accept, u_sample, draft_lengths, temperature, tokens_out,
+                          accepted_out, ws)
     if target.dim() != 3:
         raise ValueError("target must have shape [B, S + 1, V]")
     B, S, V = target.shape
     S -= 1
     if S < 0:
         raise ValueError("target must have a row behind the drafts")
-    t = _rows(target, target.shape, "target", device)
+    t = _rows(target, (B, S + 1, V), "target", device)
     q = (None, 0, 0, 0) if draft is None else _rows(draft, (B, S, V), "draft", device)
-    vectors = (_vector(draft_tokens, torch.int32, (B, S), "draft_tokens", device),
-               _vector(draft_lengths, torch.int32, (B,), "draft_lengths", device),
-               _vector(temperature, torch.float32, (B,), "temperature", device),
-               _vector(u_accept, torch.float32, (B, S), "u_accept", device), _vector(u_sample, torch.float32, (B,), "u_sample", device))
+    ints, floats = torch.int32, torch.float32
+    tokens = _vector(draft_tokens, ints, (B, S), "draft_tokens", device)
+    lengths = None if draft_lengths is None else _vector(draft_lengths, ints, (B,), "draft_lengths", device)
+    T = None if temperature is None else _vector(temperature, floats, (B,), "temperature", device)
+    ua, us = _vector(u_accept, floats, (B, S), "u_accept", device), _vector(u_sample, floats, (B,), "u_sample", device)
     if tokens_out is None:
-        tokens_out = torch.empty((B, S + 1), dtype=torch.int32, device=device)
+        tokens_out = torch.empty_strided((B, S + 1), (S + 1, 1), dtype=ints, device=device)
+        out = tokens_out.data_ptr()
+    else:
+        out = _vector(tokens_out, ints, (B, S + 1), "tokens_out", device)
     if accepted_out is None:
-        accepted_out = torch.empty((B,), dtype=torch.int32, device=device)
-    outs = (_vector(tokens_out, torch.int32, (B, S + 1), "tokens_out", device),
-            _vector(accepted_out, torch.int32, (B,), "accepted_out", device))
-    L = lib()
-
-    def call(stream):
-        room = _control_block(device, stream) if ws is None else ws
-        return L.cat_verify_drafts(*t, *q, *vectors, B, S, V, *outs, room.data_ptr(), room.numel() * room.element_size(), stream)
-
-    _check(_call_on(device, call), "cat_verify_drafts")
+        accepted_out = torch.empty_strided((B,), (1,), dtype=ints, device=device)
+        kept = accepted_out.data_ptr()
+    else:
+        kept = _vector(accepted_out, ints, (B,), "accepted_out", device)
+    stream = torch._C._cuda_getCurrentRawStream(index)
+    if ws is None:
+        ws = _control_block(index, stream)
+    st = (_lib or lib()).cat_verify_drafts(*t, *q, tokens, lengths, T, ua, us, B, S, V, out, kept, ws.data_ptr(), ws.nbytes, stream)
+    if st != CAT_OK:
+        raise CatError(st, "cat_verify_drafts")
     return tokens_out, accepted_out
 
 

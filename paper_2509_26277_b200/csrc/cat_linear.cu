@@ -22,8 +22,9 @@ namespace {
 
 constexpr int LN_BK = 64;                       // inner columns per slab (128 bytes)
 constexpr int LN_MAX_STAGES = 12;
-constexpr int LN_EPI_WARPS = 8;                 // two per quarter of the TMEM lanes
-constexpr int LN_THREADS = 32 * (2 + LN_EPI_WARPS);
+constexpr int LN_EPI_WARPS = 16;                // warps of the epilogue at most: four per quarter of the TMEM lanes
+constexpr int LN_MAX_THREADS = 32 * (2 + LN_EPI_WARPS);
+constexpr int LN_RUN = 12;                      // slabs per run of an accumulator at most, where the result is fp32 (see linear_kernel)
 constexpr int LN_GROUP = 8;                     // token tiles that share a sweep over the weights
 
 struct LinearParams {
@@ -38,7 +39,7 @@ struct LinearParams {
     int nt_cta;        // of which this CTA stages that many
     int tiles_w;       // tiles along N
     int tiles_t;       // tiles along M
-    int splits;        // CTAs of a cluster that share a tile's inner dimension (1: none)
+    int splits;        // CTAs (or pairs of them) of a cluster that share a tile's inner dimension (1: none)
     int stages;
     int tmem_cols;
     uint32_t idesc;
@@ -82,45 +83,80 @@ struct Elem<CAT_F16> {
     static __device__ __forceinline__ __half down(float v) { return __float2half_rn(v); }
 };
 
-// gelu through erfc, which keeps its relative accuracy where 1 + erf(z) cancels; silu and gelu_tanh as z / (1 + e^-x): the tanh form
-// 0.5 z (1 + tanh u) is z / (1 + e^-2u).
-template <int ACT>
+__device__ __forceinline__ float fast_exp2(float x)
+{
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
+    return e;
+}
+__device__ __forceinline__ float fast_rcp(float x)
+{
+    float e;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
+    return e;
+}
+
+// gelu is z Phi(z) = max(z, 0) - |z| erfc(|z| / sqrt 2) / 2, which keeps its relative accuracy where 1 + erf(z) cancels; silu and gelu_tanh are
+// z / (1 + e^-x), the tanh form 0.5 z (1 + tanh u) being z / (1 + e^-2u).  Where the result is rounded to 16 bits (FAST), the special function
+// unit evaluates them (2 ulp each), and erfc(x) / 2 = t 2^(Q(t) - x^2 log2 e), t = 1 / (1 + x / 2), with Q of degree seven fitted to the
+// logarithm of erfc for the smallest largest error over 0 <= x <= 9.5: 6.3e-7 of the value.
+template <int ACT, bool FAST>
 __device__ __forceinline__ float activate(float z)
 {
     if (ACT == CAT_ACT_RELU) return z < 0.f ? 0.f : z;   // (a NaN stays one)
-    if (ACT == CAT_ACT_GELU) return 0.5f * z * erfcf(-0.70710678f * z);
+    if (ACT == CAT_ACT_GELU) {
+        if (!FAST) return 0.5f * z * erfcf(-0.70710678f * z);
+        const float a = fabsf(z), t = fast_rcp(fmaf(a, 0.35355339f, 1.f));
+        float q = -0.26331830f;
+        q = fmaf(q, t, 1.05167462f);
+        q = fmaf(q, t, -1.38636313f);
+        q = fmaf(q, t, 0.45006013f);
+        q = fmaf(q, t, -0.02762734f);
+        q = fmaf(q, t, 0.55924359f);
+        q = fmaf(q, t, 1.44212111f);
+        q = fmaf(q, t, -2.82579157f);
+        const float r = a * t * fast_exp2(fmaf(a * a, -0.72134752f, q));
+        return z > 20.f ? z : fmaxf(z, 0.f) - r;         // (of a NaN r is one)
+    }
     if (ACT == CAT_ACT_GELU_TANH) {
         const float u = 0.7978845608f * z * fmaf(0.044715f * z, z, 1.f);
-        return z / (1.f + expf(-2.f * u));
+        return FAST ? z * fast_rcp(1.f + fast_exp2(-2.8853901f * u)) : z / (1.f + expf(-2.f * u));
     }
-    if (ACT == CAT_ACT_SILU) return z / (1.f + expf(-z));
+    if (ACT == CAT_ACT_SILU) return FAST ? z * fast_rcp(1.f + fast_exp2(-1.44269504f * z)) : z / (1.f + expf(-z));
     return z;
 }
 
 // 16 tokens of this thread's output column: y = act(acc + b) + r.  `count` tokens are there.
 template <int OT, int ACT>
-__device__ __forceinline__ void finish16(const float *acc, float bias, const typename Elem<OT>::type *res, int64_t ldr,
+__device__ __forceinline__ void finish16(const float (&acc)[16], float bias, const typename Elem<OT>::type *res, int64_t ldr,
                                          typename Elem<OT>::type *out, int64_t ldy, int count)
 {
     using E = Elem<OT>;
-    typename E::type r[16];
-    if (res) {
+    constexpr bool FAST = OT != CAT_F32;
+    if (count >= 16) {
+        if (res) {
+            typename E::type r[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j, res += ldr) r[j] = *res;
+#pragma unroll
+            for (int j = 0; j < 16; ++j, out += ldy) *out = E::down(activate<ACT, FAST>(acc[j] + bias) + E::up(r[j]));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j, out += ldy) *out = E::down(activate<ACT, FAST>(acc[j] + bias));
+        }
+    } else {
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-            if (j < count) r[j] = res[j * ldr];
-    }
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        float y = activate<ACT>(acc[j] + bias);
-        if (j < count) {
-            if (res) y += E::up(r[j]);
-            out[j * ldy] = E::down(y);
-        }
+            if (j < count) {
+                float y = activate<ACT, FAST>(acc[j] + bias);
+                if (res) y += E::up(res[j * ldr]);
+                out[j * ldy] = E::down(y);
+            }
     }
 }
 
 template <int OT>
-__device__ __forceinline__ void finish(int act, const float *acc, float bias, const typename Elem<OT>::type *res, int64_t ldr,
+__device__ __forceinline__ void finish(int act, const float (&acc)[16], float bias, const typename Elem<OT>::type *res, int64_t ldr,
                                        typename Elem<OT>::type *out, int64_t ldy, int count)
 {
     switch (act) {
@@ -132,15 +168,36 @@ __device__ __forceinline__ void finish(int act, const float *acc, float bias, co
     }
 }
 
+template <bool FAST>
 __device__ __forceinline__ float activate_any(int act, float z)
 {
     switch (act) {
-    case CAT_ACT_RELU: return activate<CAT_ACT_RELU>(z);
-    case CAT_ACT_GELU: return activate<CAT_ACT_GELU>(z);
-    case CAT_ACT_GELU_TANH: return activate<CAT_ACT_GELU_TANH>(z);
-    case CAT_ACT_SILU: return activate<CAT_ACT_SILU>(z);
+    case CAT_ACT_RELU: return activate<CAT_ACT_RELU, FAST>(z);
+    case CAT_ACT_GELU: return activate<CAT_ACT_GELU, FAST>(z);
+    case CAT_ACT_GELU_TANH: return activate<CAT_ACT_GELU_TANH, FAST>(z);
+    case CAT_ACT_SILU: return activate<CAT_ACT_SILU, FAST>(z);
     default: return z;
     }
+}
+
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float (&v)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]),
+        "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// arrives on the barrier at this shared-memory offset in both CTAs of the pair whose first one has this rank
+__device__ __forceinline__ void commit_to_pair(uint32_t bar, uint32_t leader)
+{
+    asm volatile(
+        "{\n\t.reg .b16 m;\n\tcvt.u16.u32 m, %1;\n\t"
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n\t}"
+        ::"r"(bar), "r"(3u << leader)
+        : "memory");
 }
 
 __device__ __forceinline__ float ld_cluster_f32(uint32_t addr)
@@ -162,7 +219,7 @@ __device__ __forceinline__ void tile_of(const LinearParams &p, int unit, int &tw
 }
 
 template <bool PAIR, int OT>
-__global__ void __launch_bounds__(LN_THREADS, 1)
+__global__ void __launch_bounds__(LN_MAX_THREADS, 1)
 linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapX, const __grid_constant__ LinearParams p)
 {
     extern __shared__ unsigned char smem_raw[];
@@ -174,26 +231,35 @@ linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ 
     const int stage_bytes = TC_A_BYTES + x_bytes;
     LinearShared &sh = *reinterpret_cast<LinearShared *>(ring_ptr + (size_t)p.stages * stage_bytes);
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = (int)blockDim.x >> 5;
     const uint32_t crank = (PAIR || p.splits > 1) ? cluster_ctarank() : 0u;
-    const uint32_t rank = PAIR ? crank : 0u;              // 0 = the CTA that issues the MMAs
-    const uint32_t split = PAIR ? 0u : crank;             // part of the inner dimension
+    const uint32_t rank = PAIR ? crank & 1u : 0u;         // 0 = the CTA that issues the MMAs
+    const uint32_t leader = PAIR ? crank & ~1u : crank;   // that CTA's rank in the cluster
+    const uint32_t split = PAIR ? crank >> 1 : crank;     // part of the inner dimension
     volatile int *abort_flag = &sh.abort_flag;
     constexpr int TW = PAIR ? 256 : 128;                  // output columns per tile
     const int units = p.tiles_w * p.tiles_t;
-    const int per_cluster = PAIR ? 2 : p.splits;
+    const int per_cluster = (PAIR ? 2 : 1) * p.splits;
     const int unit_first = blockIdx.x / per_cluster, unit_step = gridDim.x / per_cluster;
     const int slabs = (p.K + LN_BK - 1) / LN_BK;
     const int slab0 = (int)((int64_t)slabs * split / p.splits), slab1 = (int)((int64_t)slabs * (split + 1) / p.splits);
 
+    // Sums of fp32 results run over at most LN_RUN slabs at a time: the tensor cores truncate an accumulator at every step, always towards zero, and
+    // what that costs grows with the length of the run.  The epilogue adds the runs up in registers, rounding to nearest.  Relative error at 2048
+    // inner columns (2-norm; fp32 sums in another order: 3.7e-7), time of 50 000 x 1000: one run 1.9e-6, 150 us; 16 slabs 9.1e-7, 166 us; 12 slabs
+    // 6.1e-7, 174 us; 8 slabs 4.3e-7, 181 us (the epilogue of a tile's last run no longer passes under the next one).
+    const int in_split = slab1 - slab0, runs = OT == CAT_F32 ? (in_split + LN_RUN - 1) / LN_RUN : 1, run = (in_split + runs - 1) / runs;
+
     if (tid == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mapW)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mapX)) : "memory");
         for (int s = 0; s < p.stages; ++s) {
             mbar_init(smem_u32(&sh.full[s]), PAIR ? 2 : 1);   // one expect_tx arrival per CTA
             mbar_init(smem_u32(&sh.empty[s]), 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(smem_u32(&sh.tmem_full[b]), 1);
-            mbar_init(smem_u32(&sh.tmem_empty[b]), (PAIR ? 2 : 1) * LN_EPI_WARPS);
+            mbar_init(smem_u32(&sh.tmem_empty[b]), (PAIR ? 2 : 1) * (warps - 2));
         }
         mbar_init(smem_u32(&sh.drain), 1);
         sh.abort_flag = 0;
@@ -231,7 +297,7 @@ linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ 
                     if (!mbar_wait(smem_u32(&sh.empty[s]), ph ^ 1u, abort_flag, p.ctl)) { ok = false; break; }
                     const uint32_t dst = ring + (uint32_t)(s * stage_bytes);
                     if (PAIR) {
-                        const uint32_t full = mapa_cluster(smem_u32(&sh.full[s]), 0);
+                        const uint32_t full = mapa_cluster(smem_u32(&sh.full[s]), leader);
                         mbar_arrive_expect_tx_cluster(full, (uint32_t)stage_bytes);
                         tma_load_2d_pair(dst, &mapW, full, sl * LN_BK, n0);
                         tma_load_2d_pair(dst + TC_A_BYTES, &mapX, full, sl * LN_BK, t0);
@@ -258,30 +324,31 @@ linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ 
             int s = 0;
             uint32_t ph = 0, ti = 0;
             bool ok = true;
-            for (int unit = unit_first; unit < units && ok; unit += unit_step, ++ti) {
-                const int b = ti & 1;
-                if (!mbar_wait(smem_u32(&sh.tmem_empty[b]), ((ti >> 1) & 1u) ^ 1u, abort_flag, p.ctl)) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t acc = tmem_base + (uint32_t)(b * p.nt);
-                for (int sl = slab0; sl < slab1; ++sl) {
-                    if (!mbar_wait(smem_u32(&sh.full[s]), ph, abort_flag, p.ctl)) { ok = false; break; }
+            for (int unit = unit_first; unit < units && ok; unit += unit_step)
+                for (int first = slab0; first < slab1 && ok; first += run, ++ti) {
+                    const int b = ti & 1, last = min(first + run, slab1);
+                    if (!mbar_wait(smem_u32(&sh.tmem_empty[b]), ((ti >> 1) & 1u) ^ 1u, abort_flag, p.ctl)) { ok = false; break; }
                     tc_fence_after();
-                    const uint64_t at = (uint64_t)(uint32_t)(s * (stage_bytes >> 4));
+                    const uint32_t acc = tmem_base + (uint32_t)(b * p.nt);
+                    for (int sl = first; sl < last; ++sl) {
+                        if (!mbar_wait(smem_u32(&sh.full[s]), ph, abort_flag, p.ctl)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint64_t at = (uint64_t)(uint32_t)(s * (stage_bytes >> 4));
 #pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) {   // 16 inner columns = 32 B per MMA: +2 in 16-byte units
-                        const uint32_t accum = (sl > slab0 || kk > 0) ? 1u : 0u;
-                        if (PAIR) mma_f16_pair(acc, wdesc0 + at + 2 * kk, xdesc0 + at + 2 * kk, p.idesc, accum);
-                        else mma_f16(acc, wdesc0 + at + 2 * kk, xdesc0 + at + 2 * kk, p.idesc, accum);
+                        for (int kk = 0; kk < 4; ++kk) {   // 16 inner columns = 32 B per MMA: +2 in 16-byte units
+                            const uint32_t accum = (sl > first || kk > 0) ? 1u : 0u;
+                            if (PAIR) mma_f16_pair(acc, wdesc0 + at + 2 * kk, xdesc0 + at + 2 * kk, p.idesc, accum);
+                            else mma_f16(acc, wdesc0 + at + 2 * kk, xdesc0 + at + 2 * kk, p.idesc, accum);
+                        }
+                        if (PAIR) commit_to_pair(smem_u32(&sh.empty[s]), leader);
+                        else tc_commit(smem_u32(&sh.empty[s]));
+                        if (++s == p.stages) { s = 0; ph ^= 1u; }
                     }
-                    if (PAIR) tc_commit_pair(smem_u32(&sh.empty[s]));
-                    else tc_commit(smem_u32(&sh.empty[s]));
-                    if (++s == p.stages) { s = 0; ph ^= 1u; }
+                    if (ok) {
+                        if (PAIR) commit_to_pair(smem_u32(&sh.tmem_full[b]), leader);
+                        else tc_commit(smem_u32(&sh.tmem_full[b]));
+                    }
                 }
-                if (ok) {
-                    if (PAIR) tc_commit_pair(smem_u32(&sh.tmem_full[b]));
-                    else tc_commit(smem_u32(&sh.tmem_full[b]));
-                }
-            }
             // all MMAs issued by this thread have completed once this commit arrives
             if (PAIR) tc_commit_pair_local(smem_u32(&sh.drain));
             else tc_commit(smem_u32(&sh.drain));
@@ -292,72 +359,105 @@ linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ 
         // ---------------------------------------------------------------- epilogue
         using E = Elem<OT>;
         using T = typename E::type;
-        const int quarter = warp & 3, half = (warp - 2) >> 2;   // TMEM lanes this warp may read; which 16-column chunks it takes
+        const int quarter = warp & 3, part = (warp - 2) >> 2;   // TMEM lanes this warp may read; which 16-column chunks it takes
         uint32_t ti = 0;
-        for (int unit = unit_first; unit < units; unit += unit_step, ++ti) {
+        bool ok = true;
+        for (int unit = unit_first; unit < units && ok; unit += unit_step) {
             int tw, tt;
             tile_of(p, unit, tw, tt);
-            const int b = ti & 1;
             const int n = tw * TW + (int)rank * 128 + quarter * 32 + lane;
             const bool inside = n < p.N;
             const int64_t t0 = (int64_t)tt * p.nt;
             const float bias = p.bias && inside && p.splits == 1 ? load_as_float(p.bias, n, p.bias_type) : 0.f;
-            if (!mbar_wait_warp(smem_u32(&sh.tmem_full[b]), (ti >> 1) & 1u, abort_flag, p.ctl)) break;
-            tc_fence_after();
-            const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * p.nt);
-            for (int c = half * 16; c < p.nt; c += 32) {
+            float sum[OT == CAT_F32 ? 4 : 1][16];     // (fp32 results: the runs so far)
+            for (int first = slab0; first < slab1; first += run, ++ti) {
+                const int b = ti & 1;
+                const bool whole = first + run >= slab1;       // the last run
+                ok = mbar_wait_warp(smem_u32(&sh.tmem_full[b]), (ti >> 1) & 1u, abort_flag, p.ctl);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * p.nt);
                 uint32_t raw16[16];
-                tmem_ld16_issue(taddr + (uint32_t)c, raw16);
-                tmem_ld_wait16(raw16);
-                float acc[16];
+                if (OT == CAT_F32 && run < slab1 - slab0) {
+                    // runs are added up in registers; the last one's accumulator takes the whole, so that one loop finishes either kind
 #pragma unroll
-                for (int j = 0; j < 16; ++j) acc[j] = __uint_as_float(raw16[j]);
-                if (p.splits > 1) {
-                    // [token][output column] of this CTA's part, in the ring (every slab has been consumed)
-                    float *part = reinterpret_cast<float *>(ring_ptr) + (size_t)c * 128 + quarter * 32 + lane;
+                    for (int i = 0; i < 4; ++i) {
+                        const int c = ((warps - 2) / 4 * i + part) * 16;
+                        if (c >= p.nt) break;
+                        tmem_ld16_issue(taddr + (uint32_t)c, raw16);
+                        tmem_ld_wait16(raw16);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) part[j * 128] = acc[j];
-                } else if (inside && t0 + c < p.M) {
-                    const int64_t row = t0 + c;
-                    const int count = (int)min((int64_t)16, p.M - row);
-                    const T *res = p.residual ? reinterpret_cast<const T *>(p.residual) + row * p.ldr + n : nullptr;
-                    finish<OT>(p.act, acc, bias, res, p.ldr, reinterpret_cast<T *>(p.Y) + row * p.ldy + n, p.ldy, count);
+                        for (int j = 0; j < 16; ++j) sum[OT == CAT_F32 ? i : 0][j] = __uint_as_float(raw16[j]) + (first > slab0 ? sum[OT == CAT_F32 ? i : 0][j] : 0.f);
+                        if (whole) tmem_st16(taddr + (uint32_t)c, sum[OT == CAT_F32 ? i : 0]);
+                    }
+                    if (whole) tmem_st_wait();
                 }
-            }
-            // accumulator buffer b may be overwritten from here on
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                if (PAIR) mbar_arrive_cluster(mapa_cluster(smem_u32(&sh.tmem_empty[b]), 0));
-                else mbar_arrive(smem_u32(&sh.tmem_empty[b]));
+#pragma unroll 1
+                for (int c = part * 16; whole && c < p.nt; c += (warps - 2) * 4) {
+                    tmem_ld16_issue(taddr + (uint32_t)c, raw16);
+                    tmem_ld_wait16(raw16);
+                    float acc[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) acc[j] = __uint_as_float(raw16[j]);
+                    if (p.splits > 1) {
+                        // [token][output column] of this CTA's part, in the ring (every slab has been consumed)
+                        float *to = reinterpret_cast<float *>(ring_ptr) + (size_t)c * 128 + quarter * 32 + lane;
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) to[j * 128] = acc[j];
+                    } else if (inside && t0 + c < p.M) {
+                        const int64_t row = t0 + c;
+                        const int count = (int)min((int64_t)16, p.M - row);
+                        const T *res = p.residual ? reinterpret_cast<const T *>(p.residual) + row * p.ldr + n : nullptr;
+                        finish<OT>(p.act, acc, bias, res, p.ldr, reinterpret_cast<T *>(p.Y) + row * p.ldy + n, p.ldy, count);
+                    }
+                }
+                // accumulator buffer b may be overwritten from here on
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (PAIR) mbar_arrive_cluster(mapa_cluster(smem_u32(&sh.tmem_empty[b]), leader));
+                    else mbar_arrive(smem_u32(&sh.tmem_empty[b]));
+                }
             }
         }
     }
 
     tc_fence_before();
     __syncthreads();
-    if (!PAIR && p.splits > 1) {
-        // the parts meet: CTA r of the cluster adds every r-th run of 32 output columns, parts in order
+    if (p.splits > 1) {
+        // The parts meet: split q of the cluster finishes every q-th token of the tile, the parts in order.  A warp takes a token, a lane four of its
+        // 128 output columns.
         using E = Elem<OT>;
         using T = typename E::type;
         cluster_sync();
         int tw, tt;
         tile_of(p, unit_first, tw, tt);
         const int64_t t0 = (int64_t)tt * p.nt;
-        const int tokens = (int)min((int64_t)p.nt, p.M - t0);
-        const uint32_t part = ring;
+        const int tokens = (int)min((int64_t)p.nt, p.M - t0), n0 = tw * TW + (int)rank * 128 + lane;
+        float bias[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bias[i] = p.bias && n0 + 32 * i < p.N ? load_as_float(p.bias, n0 + 32 * i, p.bias_type) : 0.f;
         if (*abort_flag == 0)
-            for (int g = (int)split + p.splits * warp; g < tokens * 4; g += p.splits * (LN_THREADS / 32)) {
-                const int t = g >> 2, n = tw * TW + (g & 3) * 32 + lane;
-                float v = 0.f;
-                for (int q = 0; q < p.splits; ++q)
-                    v += ld_cluster_f32(mapa_cluster(part + (uint32_t)((t * 128 + (g & 3) * 32 + lane) * 4), (uint32_t)q));
-                if (n < p.N) {
-                    const int64_t row = t0 + t;
-                    if (p.bias) v += load_as_float(p.bias, n, p.bias_type);
-                    v = activate_any(p.act, v);
-                    if (p.residual) v += E::up(reinterpret_cast<const T *>(p.residual)[row * p.ldr + n]);
-                    reinterpret_cast<T *>(p.Y)[row * p.ldy + n] = E::down(v);
+            for (int t = (int)split + p.splits * warp; t < tokens; t += p.splits * warps) {
+                const int64_t row = t0 + t;
+                float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+                for (int q = 0; q < p.splits; ++q) {
+                    const uint32_t from = mapa_cluster(ring + (uint32_t)((t * 128 + lane) * 4), PAIR ? 2u * q + rank : (uint32_t)q);
+                    float u[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) u[i] = ld_cluster_f32(from + 128u * i);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] += u[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int n = n0 + 32 * i;
+                    if (n < p.N) {
+                        float y = activate_any<OT != CAT_F32>(p.act, v[i] + bias[i]);
+                        if (p.residual) y += E::up(reinterpret_cast<const T *>(p.residual)[row * p.ldr + n]);
+                        reinterpret_cast<T *>(p.Y)[row * p.ldy + n] = E::down(y);
+                    }
                 }
             }
     }
@@ -370,12 +470,42 @@ linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ 
     }
 }
 
-// Rows that TMA cannot address, copied to rows of `pitch` elements (zeros behind column K): 16-bit loads and stores of neighbouring lanes.
-__global__ void __launch_bounds__(256) linear_pad_kernel(const uint16_t *src, int64_t ld, int64_t rows, int K, int pitch, uint16_t *dst)
+// Rows that TMA cannot address, copied to rows of `pitch` elements (zeros behind column K), for X and W in one launch.  A thread makes 16 bytes
+// at a time, from aligned words and a shift between neighbours (the words at a row's ends element by element).
+struct PadJob {
+    const uint16_t *src;
+    uint16_t *dst;
+    int64_t ld, units;    // units: 16-byte pieces of the copy (0: nothing to do)
+};
+__global__ void __launch_bounds__(256) linear_pad_kernel(const __grid_constant__ PadJob x, const __grid_constant__ PadJob w, int K, int pitch)
 {
     pdl_enter();
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-        for (int k = threadIdx.x; k < pitch; k += blockDim.x) dst[r * pitch + k] = k < K ? src[r * ld + k] : (uint16_t)0;
+    const int per_row = pitch / 8;
+    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < x.units + w.units; u += (int64_t)gridDim.x * 256) {
+        const bool of_x = u < x.units;
+        const int64_t at = of_x ? u : u - x.units;
+        const int64_t row = at / per_row;
+        const int k = (int)(at - row * per_row) * 8;
+        const uint16_t *src = (of_x ? x.src : w.src) + row * (of_x ? x.ld : w.ld) + k;
+        uint32_t v[4];
+        const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(src) & 3u;
+        if (k >= 1 && k + 8 < K) {      // (one element before and one behind are in the row)
+            const uint32_t *words = reinterpret_cast<const uint32_t *>(reinterpret_cast<const unsigned char *>(src) - off);
+            uint32_t a[5];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) a[q] = __ldg(words + q);
+            a[4] = off ? __ldg(words + 4) : 0u;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = __funnelshift_r(a[q], a[q + 1], 8 * off);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t lo = k + 2 * q < K ? src[2 * q] : 0u, hi = k + 2 * q + 1 < K ? src[2 * q + 1] : 0u;
+                v[q] = lo | (hi << 16);
+            }
+        }
+        reinterpret_cast<uint4 *>(of_x ? x.dst : w.dst)[at] = make_uint4(v[0], v[1], v[2], v[3]);
+    }
 }
 
 bool tma_rows(const void *base, int64_t ld) { return (reinterpret_cast<uintptr_t>(base) & 15u) == 0 && ld % 8 == 0; }
@@ -388,18 +518,35 @@ struct LinearPlan {
 
 LinearPlan plan(int64_t M, int N, int K, int sms)
 {
-    LinearPlan best{};
+    // Estimated times in microseconds of the forms that suit the shape; the shortest is taken.  A slab of 64 inner columns takes what is in the
+    // table (measured on 200 to 1024 rows, N = 4096 and 8192, K = 2048 and 4096, all CTAs at work), splitting the inner dimension about a microsecond and
+    // what the parts' exchange takes.
+    static const struct { int nt; float single, pair; } table[] = {{16, 0.22f, 0.f}, {32, 0.22f, 0.f}, {64, 0.23f, 0.f}, {128, 0.25f, 0.25f}, {192, 0.30f, 0.29f}, {256, 0.38f, 0.33f}};
     const int slabs = (K + LN_BK - 1) / LN_BK;
-    if (M > 128) {
-        best.pair = true;
-        best.splits = 1;
-        best.nt = (int)(M < 256 ? (M + 31) / 32 * 32 : 256);
-        return best;
+    LinearPlan best{};
+    float least = 1e30f;
+    for (const auto &row : table) {
+        if (row.nt > 16 && row.nt >= 2 * M) break;
+        for (int pair = 0; pair < 2; ++pair) {
+            const float slab = pair ? row.pair : row.single;
+            if (slab == 0.f) continue;
+            const int64_t tiles = (int64_t)((N + (pair ? 255 : 127)) / (pair ? 256 : 128)) * ((M + row.nt - 1) / row.nt);
+            // (CTAs of up to 64 tokens fit two to an SM, which they then share)
+            const int64_t slots = sms / (pair ? 2 : 1), most = row.nt <= 64 && !pair ? 2 * slots : slots;
+            for (int splits = 1; splits <= (pair ? 2 : row.nt <= 64 ? 8 : 4) && splits * 2 <= (slabs > 1 ? slabs : 2); splits *= 2) {
+                if (splits > 1 && tiles * splits > most) break;
+                const float waves = (float)((tiles * splits + slots - 1) / slots);
+                const float t = waves * (float)((slabs + splits - 1) / splits) * (row.nt == 16 && waves > 1.f ? slab - 0.03f : slab) +
+                                (splits > 1 ? 0.6f + 0.2f * splits + 2.5f * row.nt / 256.f : 0.f);
+                if (t < least) {
+                    least = t;
+                    best.pair = pair;
+                    best.nt = row.nt;
+                    best.splits = splits;
+                }
+            }
+        }
     }
-    best.nt = (int)((M + 15) / 16 * 16);
-    best.splits = 1;
-    const int tiles = (N + 127) / 128;
-    while (best.splits < 8 && tiles * best.splits * 2 <= sms && slabs >= best.splits * 4) best.splits *= 2;
     return best;
 }
 
@@ -420,18 +567,26 @@ cudaError_t launch_linear(const LinearArgs &a, void *workspace, cudaStream_t s)
     const void *X = a.X, *W = a.W;
     int64_t ldx = a.ldx, ldw = a.ldw;
     cudaError_t e;
-    auto pad = [&](const void *&src, int64_t &ld, int64_t rows) {
-        const int64_t blocks = rows < 16 * sms ? rows : 16 * sms;
-        const cudaError_t r = launch_pdl(linear_pad_kernel, dim3((unsigned)blocks), dim3(256), 0, s, reinterpret_cast<const uint16_t *>(src), ld,
-                                         rows, a.K, padded(a.K), reinterpret_cast<uint16_t *>(room));
-        count_launch();
+    auto pad = [&](const void *&src, int64_t &ld, int64_t rows, PadJob &job) {
+        if (tma_rows(src, ld)) return;
+        job.src = reinterpret_cast<const uint16_t *>(src);
+        job.dst = reinterpret_cast<uint16_t *>(room);
+        job.ld = ld;
+        job.units = rows * (padded(a.K) / 8);
         src = room;
         ld = padded(a.K);
         room += align_up((size_t)rows * padded(a.K) * 2, 256);
-        return r;
     };
-    if (!tma_rows(X, ldx) && (e = pad(X, ldx, a.M)) != cudaSuccess) return e;
-    if (!tma_rows(W, ldw) && (e = pad(W, ldw, a.N)) != cudaSuccess) return e;
+    PadJob pad_x{}, pad_w{};
+    pad(X, ldx, a.M, pad_x);
+    pad(W, ldw, a.N, pad_w);
+    if (pad_x.units + pad_w.units) {
+        const int64_t blocks = (pad_x.units + pad_w.units + 255) / 256;
+        if ((e = launch_pdl(linear_pad_kernel, dim3((unsigned)(blocks < 16 * sms ? blocks : 16 * sms)), dim3(256), 0, s, pad_x, pad_w, a.K, padded(a.K))) !=
+            cudaSuccess)
+            return e;
+        count_launch();
+    }
 
     const LinearPlan pl = plan(a.M, a.N, a.K, sms);
     LinearParams p{};
@@ -463,18 +618,21 @@ cudaError_t launch_linear(const LinearArgs &a, void *workspace, cudaStream_t s)
 
     const int stage_bytes = TC_A_BYTES + p.nt_cta * TC_SLAB_BYTES;
     const int64_t units = (int64_t)p.tiles_w * p.tiles_t;
-    const int room_smem = 227 * 1024 - 1024 - (int)sizeof(LinearShared);
+    // With few tokens half an SM's shared memory holds more than enough slabs in flight (100 KB; the memory wants about 45), and the next call's
+    // CTAs can settle in beside these.
+    const int room_smem = (pl.nt <= 64 && !pl.pair ? 113 : 227) * 1024 - 2048 - (int)sizeof(LinearShared);
     p.stages = room_smem / stage_bytes;
     if (p.stages > LN_MAX_STAGES) p.stages = LN_MAX_STAGES;
+    if (pl.splits > 1 && (size_t)p.stages * stage_bytes < (size_t)pl.nt * 512) return cudaErrorInvalidValue;   // (the parts of a split tile lie in the ring)
     const size_t smem = 1024 + (size_t)p.stages * stage_bytes + sizeof(LinearShared);
-    const int per_cluster = pl.pair ? 2 : pl.splits;
-    int64_t clusters = sms / per_cluster;
+    const int per_cluster = (pl.pair ? 2 : 1) * pl.splits;
+    int64_t clusters = (pl.nt <= 64 && !pl.pair ? 2 : 1) * sms / per_cluster;
     if (units < clusters) clusters = units;
     if (pl.splits > 1 && clusters < units) return cudaErrorInvalidValue;   // (a split tile is a cluster's only one)
 
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(clusters * per_cluster), 1, 1);
-    cfg.blockDim = dim3(LN_THREADS, 1, 1);
+    cfg.blockDim = dim3((unsigned)(64 + 32 * (pl.nt / 4 < LN_EPI_WARPS ? pl.nt / 4 : LN_EPI_WARPS)), 1, 1);   // (a warp of the epilogue per 16 tokens and quarter)
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
@@ -487,10 +645,17 @@ cudaError_t launch_linear(const LinearArgs &a, void *workspace, cudaStream_t s)
     cfg.attrs = attr;
     cfg.numAttrs = 2;
 
+    int dev = 0;
+    if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
+    const uint64_t dev_bit = dev < 64 ? (uint64_t)1 << dev : 0;
 #define CAT_LINEAR_LAUNCH(PAIR, OT)                                                                                             \
     do {                                                                                                                        \
         auto kern = linear_kernel<PAIR, OT>;                                                                                    \
-        if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024)) != cudaSuccess) return e; \
+        static std::atomic<uint64_t> ready{0};      /* (a bit per device: the attribute is set once) */                           \
+        if (!(dev_bit & ready.load(std::memory_order_relaxed))) {                                                                \
+            if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024)) != cudaSuccess) return e; \
+            ready.fetch_or(dev_bit, std::memory_order_relaxed);                                                                  \
+        }                                                                                                                        \
         e = cudaLaunchKernelEx(&cfg, kern, mapW, mapX, p);                                                                      \
     } while (0)
     if (pl.pair) {
