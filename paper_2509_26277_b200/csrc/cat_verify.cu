@@ -113,6 +113,7 @@ struct VerifyParams {
     int chunks_t, chunks_q;   // chunks of a target row, of a draft row
     int slots;       // chunk sums a CTA holds between two exchanges
     int settle;      // undecided sequences are settled in the same kernel
+    int keep;        // there is room for the weights of two rows while they are
 };
 
 __device__ __forceinline__ const void *row_of(const void *base, int type, int64_t seq, int64_t row, int64_t seq_stride, int64_t row_stride)
@@ -306,10 +307,9 @@ __device__ __forceinline__ float sum_of(const float (&w)[N])
 struct SettleShared {
     double table[64];                       // 2^(i / 64)
     int claim[2];                           // the sequence that the cluster works on, and the row it goes on from
-    float m[2][VF_THREADS / 32];     // the warps' parts of what goes over the cluster, for two rows ...
-    double z[2][VF_THREADS / 32];
-    float cta_m[2][2];                      // ... and the CTA's (two sets in turn: an exchange is one barrier)
-    double cta_z[2][2];
+    double part[2][VF_THREADS / 32];        // the warps' parts of two sums over the cluster ...
+    double cta[2][2];                       // ... and the CTA's (two sets in turn: an exchange is one barrier)
+    float top[2][2];                        // largest logits of two rows, as far as this CTA has them
 };
 
 struct VerifyShared {
@@ -590,20 +590,22 @@ __device__ __forceinline__ int find_in_chunk(const Source &src, const Scale &sc,
 
 // ---------------------------------------------------------------- in 64 bits
 // The weights 2^((x - m) c) of N logits in fp64, logits as the definitions take them: 2^(n / 64) from a table, the rest by the Taylor series of
-// e^(r ln 2) up to the fourth power (|r| <= 1 / 128 leaves 4e-14).  Ten fp64 operations each, which is what bounds the pass (floats are made
-// doubles by moving their bits where c leaves ordinary logits ordinary numbers: the conversion unit is the slower one).  Step by step across
-// the entries, and so that the compiler keeps it that way: one alone is a chain of dependent steps.
+// e^(r ln 2) up to the fourth power (|r| <= 1 / 128 leaves 4e-14).  Ten fp64 operations each (floats are made doubles by moving their bits
+// where c leaves ordinary logits ordinary numbers: the conversion unit is slower).  Step by step across the entries, and so that the
+// compiler keeps it that way: one alone is a chain of dependent steps.
 template <int N>
 __device__ __forceinline__ void weights_f64(const double *table, const float (&x)[N], float m, double c, double (&w)[N])
 {
     double e[N], t[N], r[N];
-    bool low[N];
+    int beyond[N];
     const float cf = (float)c;
     const bool ordinary = cf > 1e-15f && cf < 1e15f;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        low[k] = !((x[k] - m) * cf > -1000.f) || x[k] == -CUDART_INF_F;      // (NaN among them)
-        const float y = low[k] ? m : fminf(x[k], VF_LARGEST);
+        const float z = x[k] != x[k] ? -CUDART_INF_F : fminf(x[k], VF_LARGEST), at = (z - m) * cf;
+        const bool fits = at > -1000.f && at < 1000.f;
+        beyond[k] = fits ? 0 : at >= 1000.f ? 2 : 1;      // (a reference that does not suit the row shows in the sum)
+        const float y = fits ? z : m;
         const uint32_t f = __float_as_uint(y);
         if (ordinary) e[k] = __hiloint2double((int)((f & 0x80000000u) | (((f & 0x7fffffffu) >> 3) + 0x38000000u)), (int)(f << 29));
         else e[k] = (double)y;
@@ -631,7 +633,7 @@ __device__ __forceinline__ void weights_f64(const double *table, const float (&x
     for (int k = 0; k < N; ++k) {
         const int n = __double2loint(t[k]);
         const double s = table[n & 63];
-        w[k] = low[k] ? 0.0 : r[k] * __hiloint2double(__double2hiint(s) + ((n >> 6) << 20), __double2loint(s));
+        w[k] = beyond[k] == 0 ? r[k] * __hiloint2double(__double2hiint(s) + ((n >> 6) << 20), __double2loint(s)) : beyond[k] == 2 ? 1e300 : 0.0;
     }
 }
 __device__ __forceinline__ void fill_table(double *table)
@@ -639,13 +641,20 @@ __device__ __forceinline__ void fill_table(double *table)
     if (threadIdx.x < 64) table[threadIdx.x] = exp2((double)threadIdx.x * 0.015625);
 }
 
-// One cluster settles a sequence in fp64: CTA r, warp w take the (warps r + w)-th part of a row's granules, in order.
+// One cluster settles a sequence in fp64.  Its rows are taken four entries at a time, both on the grid of the target's addresses: CTA r, warp w have
+// the (warps r + w)-th part, in order.
+template <int TT, int QT>
 struct Settle {
+    const VerifyArgs &a;
     SettleShared &sh;
+    double *kept;                    // [row][entry of four][unit]: the weights, where they find room (else null)
+    const void *t_row, *q_row;       // q_row: null where there is none
     int rank, size, warps, warp, lane, turn = 0;
+    int offset, g_cta, room, g_first, g_end;
+    float m[2] = {0.f, 0.f};         // what the weights of the rows are relative to
     double c;
 
-    __device__ Settle(SettleShared &s, int n, double T) : sh(s), size(n)
+    __device__ Settle(const VerifyArgs &args, SettleShared &s, double *k, int n, double T) : a(args), sh(s), kept(k), size(n)
     {
         rank = size > 1 ? (int)cta_rank() : 0;
         warps = (int)blockDim.x >> 5;
@@ -653,210 +662,215 @@ struct Settle {
         lane = threadIdx.x & 31;
         c = fmax(1.4426950408889634 / T, 1e-300);       // (T infinite: all entries that are there weigh the same)
     }
-    __device__ int first(int granules, int w) const { return (int)((int64_t)granules * (rank * warps + w) / (size * warps)); }
-    __device__ __forceinline__ double weight(float x, float m) const
+    __device__ void rows(const void *t, const void *q)
+    {
+        t_row = t;
+        q_row = q;
+        offset = fours_offset<TT>(t);
+        const int64_t units = (a.V + offset + 3) / 4, parts = (int64_t)size * warps;
+        g_cta = (int)(units * rank / size);
+        room = (int)((units + size - 1) / size);
+        g_first = (int)(units * (rank * warps + warp) / parts);
+        g_end = (int)(units * (rank * warps + warp + 1) / parts);
+        m[0] = m[1] = 0.f;
+    }
+    __device__ __forceinline__ double weight(float x, float ref) const
     {
         const float xs[1] = {x};
         double w[1];
-        weights_f64<1>(sh.table, xs, m, c, w);
+        weights_f64<1>(sh.table, xs, ref, c, w);
         return w[0];
     }
-    // sums over the cluster, in a fixed order
-    __device__ double sum(double v)
+    // two sums over the cluster, in a fixed order; their parts stay in sh.part and sh.cta[turn]
+    __device__ void sums(double &v0, double &v1)
     {
         turn ^= 1;
-        v = warp_sum(v);
-        if (lane == 0) sh.z[0][warp] = v;
-        __syncthreads();
-        if (warp == 0) {
-            v = warp_sum(lane < warps ? sh.z[0][lane] : 0.0);
-            if (lane == 0) sh.cta_z[turn][0] = v;
-        }
-        sync_cluster();
-        return warp_sum(lane < size ? peer_f64(&sh.cta_z[turn][0], (uint32_t)lane) : 0.0);
-    }
-    // the lanes' (m, z) pairs -- largest logit, sum of weights relative to it -- joined
-    __device__ __forceinline__ void join(float &m, double &z) const
-    {
-        const float top = warp_max(m);
-        z = warp_sum(m > -CUDART_INF_F ? z * weight(m, top) : 0.0);
-        m = top;
-    }
-    // four logits into a lane's pair
-    __device__ __forceinline__ void take(const float (&x)[4], float &m, double &z) const
-    {
-        const float top = fmaxf(m, fminf(fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), -CUDART_INF_F), VF_LARGEST));
-        if (top == -CUDART_INF_F) return;
-        if (m > -CUDART_INF_F && top > m) z *= weight(m, top);
-        double w[4];
-        weights_f64<4>(sh.table, x, top, c, w);
-        z += (w[0] + w[1]) + (w[2] + w[3]);
-        m = top;
-    }
-    template <int TYPE>
-    __device__ __forceinline__ void read(const void *row, int V, float &m, double &z) const
-    {
-        m = -CUDART_INF_F;
-        z = 0;
-        const int offset = fours_offset<TYPE>(row), units = (V + offset + 3) / 4, end = first(units, warp + 1);
-        int g = first(units, warp) + lane;
-        Words<Logits<TYPE>::SIZE> v = words_of<TYPE, 4>(row, g < end ? g * 4 - offset : -4, V);
-#pragma unroll 1
-        for (; g < end; g += 32) {
-            const Words<Logits<TYPE>::SIZE> next = words_of<TYPE, 4>(row, g + 32 < end ? (g + 32) * 4 - offset : -4, V);
-            float x[4];
-            entries<TYPE, 4>(v, x);
-            take(x, m, z);
-            v = next;
-        }
-    }
-    // largest logits and sums of weights of a target row and (if there is one) a draft row
-    template <int TT, int QT>
-    __device__ void normalisers(const void *t_row, const void *q_row, int V, float (&m)[2], double (&z)[2])
-    {
-        read<TT>(t_row, V, m[0], z[0]);
-        m[1] = -CUDART_INF_F;
-        z[1] = 0;
-        if (q_row) read<QT>(q_row, V, m[1], z[1]);
-        turn ^= 1;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            join(m[i], z[i]);
-            if (lane == 0) {
-                sh.m[i][warp] = m[i];
-                sh.z[i][warp] = z[i];
-            }
+        const double s0 = warp_sum(v0), s1 = warp_sum(v1);
+        if (lane == 0) {
+            sh.part[0][warp] = s0;
+            sh.part[1][warp] = s1;
         }
         __syncthreads();
         if (warp < 2) {
-            const bool there = lane < warps;
-            float M = there ? sh.m[warp][lane] : -CUDART_INF_F;
-            double Z = there ? sh.z[warp][lane] : 0.0;
-            join(M, Z);
-            if (lane == 0) {
-                sh.cta_m[turn][warp] = M;
-                sh.cta_z[turn][warp] = Z;
-            }
+            const double s = warp_sum(lane < warps ? sh.part[warp][lane] : 0.0);
+            if (lane == 0) sh.cta[turn][warp] = s;
         }
         sync_cluster();
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const bool there = lane < size;
-            m[i] = there ? peer_f32(&sh.cta_m[turn][i], (uint32_t)lane) : -CUDART_INF_F;
-            z[i] = there ? peer_f64(&sh.cta_z[turn][i], (uint32_t)lane) : 0.0;
-            join(m[i], z[i]);
+        v0 = warp_sum(lane < size ? peer_f64(&sh.cta[turn][0], (uint32_t)lane) : 0.0);
+        v1 = warp_sum(lane < size ? peer_f64(&sh.cta[turn][1], (uint32_t)lane) : 0.0);
+    }
+    // the weights of one unit of both rows
+    __device__ __forceinline__ void weights_at(int g, double (&wt)[4], double (&wq)[4]) const
+    {
+        const int i = g * 4 - offset;
+        const Words<Logits<TT>::SIZE> tv = words_of<TT, 4>(t_row, i, a.V);
+        Words<Logits<QT>::SIZE> qv;
+        if (q_row) qv = words_of<QT, 4>(q_row, i, a.V);
+        float x[4];
+        entries<TT, 4>(tv, x);
+        weights_f64<4>(sh.table, x, m[0], c, wt);
+        if (q_row) {
+            entries<QT, 4>(qv, x);
+            weights_f64<4>(sh.table, x, m[1], c, wq);
+        } else {
+            wq[0] = wq[1] = wq[2] = wq[3] = 0;
         }
+    }
+    __device__ __forceinline__ void weights_kept(int g, double (&wt)[4], double (&wq)[4]) const
+    {
+        if (!kept) {
+            weights_at(g, wt, wq);
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            wt[k] = kept[k * room + g - g_cta];
+            wq[k] = q_row ? kept[(4 + k) * room + g - g_cta] : 0.0;
+        }
+    }
+    // sums of the rows' weights
+    __device__ void normalisers(double &zt, double &zq)
+    {
+        for (int attempt = 0;; ++attempt) {
+            zt = zq = 0;
+#pragma unroll 1
+            for (int g = g_first + lane; g < g_end; g += 32) {
+                double wt[4], wq[4];
+                weights_at(g, wt, wq);
+                zt += (wt[0] + wt[1]) + (wt[2] + wt[3]);
+                zq += (wq[0] + wq[1]) + (wq[2] + wq[3]);
+                if (kept) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        kept[k * room + g - g_cta] = wt[k];
+                        if (q_row) kept[(4 + k) * room + g - g_cta] = wq[k];
+                    }
+                }
+            }
+            sums(zt, zq);
+            // With logits / T within some hundreds of zero, nought is as good a reference as the row's largest.  Else they are looked up.
+            const bool suits = zt > 1e-200 && zt < 1e270 && (!q_row || (zq > 1e-200 && zq < 1e270));
+            if (suits || attempt == 1) return;
+            m[0] = largest<TT>(t_row, 0);
+            m[1] = q_row ? largest<QT>(q_row, 1) : 0.f;
+            if (m[0] == -CUDART_INF_F) m[0] = 0.f;
+            if (m[1] == -CUDART_INF_F) m[1] = 0.f;
+        }
+    }
+    template <int TYPE>
+    __device__ float largest(const void *row, int which)
+    {
+        float top = -CUDART_INF_F;
+#pragma unroll 1
+        for (int g = g_first + lane; g < g_end; g += 32) {
+            float x[4];
+            entries<TYPE, 4>(words_of<TYPE, 4>(row, g * 4 - offset, a.V), x);
+            top = fmaxf(top, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
+        }
+        top = fminf(warp_max(top), VF_LARGEST);
+        if (lane == 0) sh.part[which][warp] = (double)top;
+        turn ^= 1;
+        __syncthreads();
+        if (warp == 0) {
+            const float t = warp_max(lane < warps ? (float)sh.part[which][lane] : -CUDART_INF_F);
+            if (lane == 0) sh.top[turn][which] = t;
+        }
+        sync_cluster();
+        return warp_max(lane < size ? peer_f32(&sh.top[turn][which], (uint32_t)lane) : -CUDART_INF_F);
     }
 };
 
 // Sequence b from its row j on (the drafts before stand), by the whole cluster.  Greedy sequences never come here.
 template <int TT, int QT>
-__device__ __noinline__ void settle_sequence(const VerifyParams &p, SettleShared &sh, int size, int b, int j)
+__device__ __noinline__ void settle_sequence(const VerifyParams &p, SettleShared &sh, double *kept, int size, int b, int j)
 {
-    using L = Logits<TT>;
     const VerifyArgs &a = p.a;
     const int length = a.lengths ? min(a.lengths[b], a.S) : a.S;
-    Settle c(sh, size, a.temperature ? (double)a.temperature[b] : 1.0);
+    Settle<TT, QT> c(a, sh, kept, size, a.temperature ? (double)a.temperature[b] : 1.0);
+    const int lane = c.lane;
     const bool writer = c.rank == 0 && threadIdx.x == 0;
-    fill_table(sh.table);
-    __syncthreads();
     if (writer) atomicAdd(reinterpret_cast<unsigned long long *>(&p.ctl->refined_total), 1ull);
     int32_t *out = a.tokens_out + (int64_t)b * (a.S + 1);
-    const void *t_row, *q_row;
-    float m[2];
-    double z[2];
+    double zt, zq;
     int x = -1;
     bool refused = false;
     for (;; ++j) {
-        t_row = row_of(a.target, TT, b, j, a.target_seq, a.target_row);
-        q_row = a.draft && j < length ? row_of(a.draft, QT, b, j, a.draft_seq, a.draft_row) : nullptr;
-        c.normalisers<TT, QT>(t_row, q_row, a.V, m, z);
+        c.rows(row_of(a.target, TT, b, j, a.target_seq, a.target_row),
+               a.draft && j < length ? row_of(a.draft, QT, b, j, a.draft_seq, a.draft_row) : nullptr);
+        c.normalisers(zt, zq);
         if (j == length) break;
         x = a.tokens[(int64_t)b * a.S + j];
         const bool inside = x >= 0 && x < a.V;
         // u q < p, both sides times both normalisers
         double p_x = 0, q_x = 0;
-        if (inside && z[0] > 0) p_x = c.weight(logit(t_row, x, TT), m[0]) * (z[1] > 0 ? z[1] : 1.0);
-        if (!a.draft) q_x = inside ? z[0] : 0.0;
-        else if (inside && z[1] > 0) q_x = c.weight(logit(q_row, x, QT), m[1]) * z[0];
+        if (inside && zt > 0) p_x = c.weight(logit(c.t_row, x, TT), c.m[0]) * (zq > 0 ? zq : 1.0);
+        if (!a.draft) q_x = inside ? zt : 0.0;
+        else if (inside && zq > 0) q_x = c.weight(logit(c.q_row, x, QT), c.m[1]) * zt;
         refused = !(uniform(a.u_accept[(int64_t)b * a.S + j]) * q_x < p_x);
         if (refused) break;
         if (writer) out[j] = x;
     }
     int token = -1;
     bool mine = writer;
-    if (z[0] > 0) {
-        const double per_t = 1.0 / z[0], per_q = z[1] > 0 ? 1.0 / z[1] : 0.0;
-        bool residual = refused;
-        // masses of four entries from i on
-        auto masses = [&](int i, double (&w)[4]) {
-            const Words<L::SIZE> tv = words_of<TT, 4>(t_row, i, a.V);
-            const bool less = residual && per_q > 0;
-            Words<Logits<QT>::SIZE> qv;
-            if (less) qv = words_of<QT, 4>(q_row, i, a.V);
-            float y[4];
-            entries<TT, 4>(tv, y);
-            weights_f64<4>(sh.table, y, m[0], c.c, w);
+    if (zt > 0) {
+        // Masses: the target's weights as they are, or (residual) what the draft's row leaves of p; the sums of the former are there.
+        const double per_t = 1.0 / zt, per_q = zq > 0 ? 1.0 / zq : 0.0;
+        bool residual = refused && (zq > 0 || !a.draft);
+        auto masses = [&](int g, double (&w)[4]) {
+            double wq[4];
+            c.weights_kept(g, w, wq);
+            if (!residual) return;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] *= per_t;
-            if (less) {
-                double u[4];
-                entries<QT, 4>(qv, y);
-                weights_f64<4>(sh.table, y, m[1], c.c, u);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    w[k] = fma(u[k], -per_q, w[k]);
-                    if (__double2hiint(w[k]) < 0) w[k] = 0.0;
-                }
+            for (int k = 0; k < 4; ++k) {
+                w[k] = fma(wq[k], -per_q, w[k] * per_t);
+                if (__double2hiint(w[k]) < 0 || (!a.draft && g * 4 - c.offset + k == x)) w[k] = 0.0;
             }
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (i + k < 0 || i + k >= a.V || (residual && !a.draft && i + k == x)) w[k] = 0.0;
         };
-        const int offset = fours_offset<TT>(t_row), units = (a.V + offset + 3) / 4;
-        const int g_first = c.first(units, c.warp), g_end = c.first(units, c.warp + 1);
-        double total = 0;
+        double total = zt;
+        if (residual) {
+            double none = 0;
+            total = 0;
 #pragma unroll 1
-        for (int attempt = 0; attempt < 2; ++attempt) {
-            double part = 0;
-#pragma unroll 1
-            for (int g = g_first + c.lane; g < g_end; g += 32) {
+            for (int g = c.g_first + lane; g < c.g_end; g += 32) {
                 double w[4];
-                masses(g * 4 - offset, w);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) part += w[k];
+                masses(g, w);
+                total += (w[0] + w[1]) + (w[2] + w[3]);
             }
-            total = c.sum(part);
-            if (!residual || total >= VF_NO_RESIDUAL) break;
-            residual = false;
+            c.sums(total, none);
+            if (total < VF_NO_RESIDUAL) {
+                residual = false;
+                total = 0;
+#pragma unroll 1
+                for (int g = c.g_first + lane; g < c.g_end; g += 32) {
+                    double w[4];
+                    masses(g, w);
+                    total += (w[0] + w[1]) + (w[2] + w[3]);
+                }
+                c.sums(total, none);
+            }
         }
         // the CTA, the warp, the entry at which the sum passes u times the whole; roundings apart: the last with mass
         const double goal = uniform(a.u_sample[b]) * total;
         auto passes = [&](double v, double &below) {
-            const double run = warp_scan(v, c.lane);
+            const double run = warp_scan(v, lane);
             const unsigned over = __ballot_sync(0xffffffffu, v > 0 && below + run > goal), any = __ballot_sync(0xffffffffu, v > 0);
             const int l = over ? __ffs(over) - 1 : 31 - __clz(any);
             below += __shfl_sync(0xffffffffu, run - v, l);
             return l;
         };
         double below = 0;
-        const int owner = passes(c.lane < size ? peer_f64(&sh.cta_z[c.turn][0], (uint32_t)c.lane) : 0.0, below);
+        const int owner = passes(lane < size ? peer_f64(&sh.cta[c.turn][0], (uint32_t)lane) : 0.0, below);
         mine = false;
         if (owner == c.rank) {
-            const int owner_warp = passes(c.lane < c.warps ? sh.z[0][c.lane] : 0.0, below);
+            const int owner_warp = passes(lane < c.warps ? sh.part[0][lane] : 0.0, below);
             if (owner_warp == c.warp) {
                 int some = -1;
 #pragma unroll 1
-                for (int base = g_first; base < g_end && token < 0; base += 32) {
-                    const int g = base + c.lane, i = g * 4 - offset;
-                    double w[4], sum = 0;
-                    masses(i, w);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if (g >= g_end) w[k] = 0;       // (the next warp's)
-                        sum += w[k];
-                    }
-                    const double run = warp_scan(sum, c.lane);
+                for (int base = c.g_first; base < c.g_end && token < 0; base += 32) {
+                    const int g = base + lane, i = g * 4 - c.offset;
+                    double w[4] = {0, 0, 0, 0};
+                    if (g < c.g_end) masses(g, w);
+                    const double sum = (w[0] + w[1]) + (w[2] + w[3]), run = warp_scan(sum, lane);
                     int here = -1, last = -1;
                     double at = below + run - sum;
 #pragma unroll
@@ -873,7 +887,7 @@ __device__ __noinline__ void settle_sequence(const VerifyParams &p, SettleShared
                     below += __shfl_sync(0xffffffffu, run, 31);
                 }
                 if (token < 0) token = some;
-                mine = c.lane == 0;
+                mine = lane == 0;
             }
         }
     }
@@ -891,7 +905,9 @@ constexpr int VF_CLAIMED = -(1 << 30);
 template <int TT, int QT>
 __global__ void __launch_bounds__(VF_THREADS, 1) verify_settle_kernel(const __grid_constant__ VerifyParams p)
 {
+    extern __shared__ double kept[];
     __shared__ SettleShared sh;
+    fill_table(sh.table);     // (while the kernel before this one ends)
     pdl_enter();
     const VerifyArgs &a = p.a;
     const int clusters = (int)gridDim.x / p.size, own = (int)blockIdx.x / p.size, lane = threadIdx.x & 31;
@@ -926,7 +942,7 @@ __global__ void __launch_bounds__(VF_THREADS, 1) verify_settle_kernel(const __gr
         sync_cluster();
         const int b = peer_s32(&sh.claim[0], 0), row = peer_s32(&sh.claim[1], 0);
         if (b < 0) break;
-        settle_sequence<TT, QT>(p, sh, p.size, b, row);      // (its barriers lie between this claim's reading and the next one's writing)
+        settle_sequence<TT, QT>(p, sh, p.keep ? kept : nullptr, p.size, b, row);      // (its barriers lie between this claim's reading and the next one's writing)
     }
     sync_cluster();
 }
@@ -1211,7 +1227,11 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
     if (p.settle) {
         const bool open = verdict == VF_UNDECIDED || peer_s32(&sh.open, (uint32_t)sh.owner) != 0;
         if (size > 1) sync_cluster();
-        if (open) settle_sequence<TT, QT>(p, sh.settle, size, b, j);
+        if (open) {
+            fill_table(sh.settle.table);
+            __syncthreads();
+            settle_sequence<TT, QT>(p, sh.settle, p.keep ? chunk_z : nullptr, size, b, j);
+        }
     }
 }
 
@@ -1231,6 +1251,7 @@ cudaError_t launch_settle(const VerifyParams &p, cudaLaunchConfig_t &cfg)
 {
     cudaError_t e;
     if ((e = cudaFuncSetAttribute(verify_settle_kernel<TT, QT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
+    if ((e = cudaFuncSetAttribute(verify_settle_kernel<TT, QT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024)) != cudaSuccess) return e;
     return cudaLaunchKernelEx(&cfg, verify_settle_kernel<TT, QT>, p);
 }
 
@@ -1269,11 +1290,16 @@ cudaError_t launch_verify(const VerifyArgs &a, void *workspace, cudaStream_t s)
     // An undecided sequence is settled by the CTAs that have it where four passes over a row do; else by a cluster of 16 in a launch of its own
     // (64 sequences, V = 128 000: 116 us against 142; 256 sequences, V = 50 001: 39 us against 88).
     p.settle = entries <= (int64_t)16 * VF_THREADS * p.size;
+    // (the weights of two rows in fp64: where a CTA has an SM to itself, or they are small)
+    auto kept_bytes = [&](int size) { return ((entries + 6) / 4 / size + 1) * 64; };
+    size_t smem = (size_t)p.slots * 12;
+    p.keep = p.settle && (kept_bytes(p.size) <= 16 * 1024 || ((int64_t)a.B * p.size <= sms && kept_bytes(p.size) <= 200 * 1024));
+    if (p.keep && smem < (size_t)kept_bytes(p.size)) smem = (size_t)kept_bytes(p.size);
 
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(a.B * p.size), 1, 1);
     cfg.blockDim = dim3(VF_THREADS, 1, 1);
-    cfg.dynamicSmemBytes = (size_t)p.slots * 12;
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -1295,10 +1321,11 @@ cudaError_t launch_verify(const VerifyArgs &a, void *workspace, cudaStream_t s)
     if (e != cudaSuccess || p.settle) return e;
 
     p.size = VF_MAX_CLUSTER;
+    p.keep = kept_bytes(p.size) <= 200 * 1024;
     const int clusters = a.B < sms / p.size ? a.B : sms / p.size;
     cfg.gridDim = dim3((unsigned)(clusters * p.size), 1, 1);
     cfg.blockDim = dim3(VF_THREADS, 1, 1);
-    cfg.dynamicSmemBytes = 0;
+    cfg.dynamicSmemBytes = p.keep ? (size_t)kept_bytes(p.size) : 0;
     attr[0].val.clusterDim.x = (unsigned)p.size;
     e = settle[a.target_type][draft_type](p, cfg);
     count_launch();
