@@ -29,7 +29,6 @@ namespace {
 constexpr int VF_THREADS = 512;
 constexpr int VF_MAX_CLUSTER = 16;
 constexpr double VF_NO_RESIDUAL = 9.094947017729282e-13;   // 2^-40: a residual of less mass is what rounding left of none
-constexpr float VF_LARGEST = 3.4028234663852886e38f;
 
 __device__ __forceinline__ uint32_t cta_rank()
 {
@@ -67,8 +66,12 @@ __device__ __forceinline__ int peer_s32(const int *p, uint32_t rank)
     return v;
 }
 
-// A logit as the definitions take it: NaN counts as -inf, +inf as the largest number.
-__device__ __forceinline__ float clean(float x) { return fminf(x != x ? -CUDART_INF_F : x, VF_LARGEST); }
+// A logit as the definitions take it: NaN counts as -inf, +inf as the largest number. 
+__device__ __forceinline__ float clean(float x)
+{
+    const uint32_t u = __float_as_uint(x), size = u & 0x7fffffffu;
+    return __uint_as_float(size > 0x7f800000u ? 0xff800000u : u == 0x7f800000u ? 0x7f7fffffu : u);
+}
 
 __device__ __forceinline__ float logit(const void *row, int i, int type)
 {
@@ -405,7 +408,7 @@ template <int TYPE, int VECS>
 __device__ __forceinline__ void chunk_top(const uint4 (&v)[VECS], int first, int lane, double &value, int &place)
 {
     using L = Logits<TYPE>;
-    const float m = fminf(chunk_max<TYPE, VECS>(v), VF_LARGEST);
+    const float m = clean(chunk_max<TYPE, VECS>(v));
     place = 0x7fffffff;
 #pragma unroll
     for (int q = VECS - 1; q >= 0; --q)
@@ -602,7 +605,7 @@ __device__ __forceinline__ void weights_f64(const double *table, const float (&x
     const bool ordinary = cf > 1e-15f && cf < 1e15f;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        const float z = x[k] != x[k] ? -CUDART_INF_F : fminf(x[k], VF_LARGEST), at = (z - m) * cf;
+        const float z = clean(x[k]), at = (z - m) * cf;
         const bool fits = at > -1000.f && at < 1000.f;
         beyond[k] = fits ? 0 : at >= 1000.f ? 2 : 1;      // (a reference that does not suit the row shows in the sum)
         const float y = fits ? z : m;
@@ -767,7 +770,7 @@ struct Settle {
             entries<TYPE, 4>(words_of<TYPE, 4>(row, g * 4 - offset, a.V), x);
             top = fmaxf(top, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
         }
-        top = fminf(warp_max(top), VF_LARGEST);
+        top = clean(warp_max(top));
         if (lane == 0) sh.part[which][warp] = (double)top;
         turn ^= 1;
         __syncthreads();
@@ -961,12 +964,14 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
     const float Tf = a.temperature ? a.temperature[b] : 1.f;
     const int length = a.lengths ? min(a.lengths[b], a.S) : a.S;
     if (length < 0) return;                 // (all CTAs of the cluster)
-    const bool greedy = !(Tf > 0.f);
+    // (These conditions live through the whole kernel.  They are kept in registers on purpose: as conditions, `drafts` was seen lost on the way to
+    // its last uses -- CUDA 12.9, sm_100a; test_types fails then.)
+    int greedy = !(Tf > 0.f), decides = warp == warps - 1, drafts = a.draft != nullptr && !greedy;
+    asm volatile("" : "+r"(greedy), "+r"(decides), "+r"(drafts));
     // chunks of this CTA: of target rows, of draft rows
     const int c0 = (int)((int64_t)p.chunks_t * rank / size), mine = (int)((int64_t)p.chunks_t * (rank + 1) / size) - c0;
     const int d0 = (int)((int64_t)p.chunks_q * rank / size), mine_q = (int)((int64_t)p.chunks_q * (rank + 1) / size) - d0;
     int *chunk_m = reinterpret_cast<int *>(chunk_z + p.slots);
-    const bool drafts = a.draft != nullptr && !greedy;
     auto target_row = [&](int j) { return row_of(a.target, TT, b, j, a.target_seq, a.target_row); };
     auto draft_row = [&](int j) { return row_of(a.draft, QT, b, j, a.draft_seq, a.draft_row); };
     const Scale sc(greedy ? 1.0 : (double)Tf);
@@ -981,19 +986,17 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
         group = min(2 * group, p.max_group);
         const int pairs = min(rows_t, length - j0), rows = rows_t + (drafts ? pairs : 0);
         const int tasks_t = rows_t * mine, tasks = tasks_t + (rows - rows_t) * mine_q;
-        // what the decisions take besides the sums, on its way while the rows are read
+        // What the decisions take besides the sums is read by the warp that decides, the last one: it has the fewest chunks.
         int x = -1;
         float ua = 0.f, xt = -CUDART_INF_F, xq = -CUDART_INF_F;
-        if (warp == 0 && lane < pairs) {
+        if (decides && lane < pairs) {
             x = a.tokens[(int64_t)b * a.S + j0 + lane];
             ua = a.u_accept[(int64_t)b * a.S + j0 + lane];
-        }
-        auto logits_at_drafts = [&]() {
-            if (lane < pairs && x >= 0 && x < a.V && !greedy) {
+            if (x >= 0 && x < a.V) {
                 xt = logit(target_row(j0 + lane), x, TT);
-                if (drafts) xq = logit(draft_row(j0 + lane), x, QT);
+                if (a.draft) xq = logit(draft_row(j0 + lane), x, QT);
             }
-        };
+        }
         // a warp's tasks are every warps-th chunk of the rows, one after the other
         int row_at = 0, per = mine, c = warp;
         const void *row = target_row(j0);
@@ -1022,9 +1025,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
                 chunk_z[task] = z;
                 chunk_m[task] = m;
             }
-            if (task == 0) logits_at_drafts();
         }
-        if (warp == 0 && tasks == 0) logits_at_drafts();      // (a CTA without a chunk decides as the others do)
         __syncthreads();
         // the lanes' (exponent, sum) pairs -- greedy: (place, value) -- joined
         auto join = [&](int &m, double &z) {
@@ -1077,7 +1078,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
             }
         }
         __syncthreads();
-        if (warp == 0) {
+        if (decides) {
             // lane i: draft j0 + i; every CTA of the cluster decides the same from the same numbers
             int how = VF_ALL_STAND;      // (nothing left to decide)
             if (lane < pairs) {
@@ -1098,16 +1099,23 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
                     const Weights wt(sc, clear ? mt : 0), wq(sc, clear ? mq : 0);
                     wt(sc, xt, xt, w[0], none);
                     wq(sc, xq, xq, w[1], none);
-                    // (an entry far below its row's largest may weigh as more than it does: the fp64 pass says)
                     if (xt == -CUDART_INF_F) w[0] = 0.f;
-                    else if (!(w[0] > 1e-27f)) clear = false;
                     if (xq == -CUDART_INF_F) w[1] = 0.f;
-                    else if (!(w[1] > 1e-27f)) clear = false;
                     if (!drafts) w[1] = x >= 0 && x < a.V ? 1.f : 0.f;
                     // u q < p, both sides times both normalisers
-                    const double left = uniform(ua) * (double)w[1] * zt, right = (double)w[0] * zq;
-                    if (fabs(left - right) < 2.0 * VF_EPS_P * (left + right)) clear = false;
-                    how = !clear ? VF_UNDECIDED : left < right ? VF_GO_ON : VF_REFUSED;
+                    const double u = uniform(ua), left = u * (double)w[1] * zt, right = (double)w[0] * zq;
+                    if (!clear) {
+                        how = VF_UNDECIDED;
+                    } else if (w[0] == 0.f) {
+                        how = VF_REFUSED;
+                    } else if (w[0] < 1e-27f || (w[1] > 0.f && w[1] < 1e-27f)) {
+                        // entries far below their rows' largest, where weights have a floor: by their exponents, as far as fp64 has such numbers
+                        const double et = (double)xt * sc.c - (double)mt, eq = drafts && w[1] > 0.f ? (double)xq * sc.c - (double)mq : 0.0;
+                        const double by = w[1] > 0.f ? et + (double)log2f((float)zq) - eq - (double)log2f((float)(u * zt)) : 1.0;
+                        how = !(et > -900.0 && eq > -900.0 && fabs(by) > 1e-3) ? VF_UNDECIDED : by > 0 ? VF_GO_ON : VF_REFUSED;
+                    } else {
+                        how = fabs(left - right) < 2.0 * VF_EPS_P * (left + right) ? VF_UNDECIDED : left < right ? VF_GO_ON : VF_REFUSED;
+                    }
                 }
             }
             const unsigned stops = __ballot_sync(0xffffffffu, how != VF_GO_ON);    // (lane `pairs` says that there is nothing left)

@@ -243,6 +243,34 @@ def test_offsets_beyond_32_bits():
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("b,s,v,dtype", [(1, 1, 1 << 22, F32), (2, 2, 1_000_003, BF), (3, 0, 600_001, FH), (40, 1, 300_000, BF)])
+def test_large_vocabularies(b, s, v, dtype):
+    agree(problem(b, s, v, dtype, dtype))
+
+
+@pytest.mark.parametrize("v", [600, 20_000, 40_000, 90_000])
+def test_both_passes_are_reached(v):
+    """Flat rows: fp32 sums leave draws undecided; the fp64 pass settles them, in the same launch or in one of its own."""
+    ws = torch.zeros(256, dtype=torch.uint8, device="cuda")
+    p = problem(200, 1, v, F32, F32, sharp=0.1, noise=0.05, greedy_every=0)
+    got = B.cat_verify_drafts(**p, ws=ws)
+    agree(p, got=got)
+    settled = B.cat_workspace_report(ws)["refined_rows_total"]
+    assert (0 < settled < 200) if v > 600 else settled < 200
+    B.cat_verify_drafts(**dict(p, target=p["target"] * 300, draft=p["draft"] * 300), ws=ws)       # peaked: hardly any
+    assert B.cat_workspace_report(ws)["refined_rows_total"] - settled < 20
+    wild = dict(p, target=p["target"] * 1e30, draft=p["draft"] * 1e30)                            # beyond what fp32 exponents hold: all
+    agree(wild, got=B.cat_verify_drafts(**wild, ws=ws))
+
+
+def test_an_output_among_the_inputs_is_refused():
+    p = problem(1, 3, 100, BF, BF)
+    both = torch.zeros((1, 4), dtype=torch.int32, device="cuda")
+    with pytest.raises(B.CatError) as e:
+        B.cat_verify_drafts(**dict(p, draft_tokens=both[:, :3]), tokens_out=both)
+    assert e.value.status == 2
+
+
 def test_refusals_on_the_device():
     p = problem(4, 2, 100, BF, BF)
     for key, bad, error in [("draft_tokens", p["draft_tokens"].long(), TypeError), ("draft_tokens", p["draft_tokens"][:, :1], ValueError),
