@@ -388,7 +388,7 @@ cat_status_t cat_linear(const void *X, int64_t ldx, const void *W, int64_t ldw, 
  * how many drafts stand and draws the token that follows them, such that the tokens are distributed as if the target had drawn
  * them one by one.  A sequence without drafts is plain sampling from its row (which is how drafts are drawn).
  *   p_j = softmax(target[b,j,:] / T_b), q_j = softmax(draft[b,j,:] / T_b)
- *   draft j is accepted iff  u_accept[b,j] q_j(x_j) < p_j(x_j);  the first one that is not ends the sequence, and the next
+ *   draft j is accepted iff  u_accept[b,j] q_j(x_j) < p_j(x_j) ;  the first one that is not ends the sequence, and the next
  *   token is drawn from max(p_j - q_j, 0);  if all are accepted it is drawn from the row behind the last.
  *   A draw is the first index at which the cumulated mass exceeds u_sample[b] times the whole mass.
  * target [B, S+1, V] and draft [B, S, V] of any of the three types each; rows target_row / draft_row elements apart (at least V),
@@ -399,7 +399,7 @@ cat_status_t cat_linear(const void *X, int64_t ldx, const void *W, int64_t ldw, 
  * all mass on the row's largest entry, the lowest index of equal ones; NaN counts as 0.  u_accept [B, S], u_sample [B]: uniform
  * numbers in [0, 1), given, so that a call is reproducible (others are brought into [0, 1 - 2^-24], NaN counts as 0).
  * tokens_out [B, S+1]: the accepted drafts, the drawn token, -1 behind it.  accepted_out [B]: how many were accepted.
- * Logits: -inf (a mask) and NaN have no mass, +inf counts as the largest finite number.  A row without any mass accepts
+ * Logits: -inf (a mask) and NaN have no mass, nor has what is below 2^-1000 of its row's largest; +inf counts as the largest finite number.  A row without any mass accepts
  * nothing and gives token -1.  A residual of less mass than 2^-40 is what rounding left of none: the draw is from p_j then.
  * The outputs are those of fp64 arithmetic: what fast fp32 sums cannot decide within their error bound goes to an fp64 pass
  * (cat_workspace_report counts those sequences).  S = 0 is allowed (draft, draft_tokens and u_accept may be NULL then), B = 0 does nothing.

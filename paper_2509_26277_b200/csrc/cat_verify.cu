@@ -760,6 +760,13 @@ struct Settle {
             if (m[1] == -CUDART_INF_F) m[1] = 0.f;
         }
     }
+    // whether a logit's weight is less than 2^-1000 of its row's largest, which is between the row's sum and a V-th (2^-22) of it
+    template <int TYPE>
+    __device__ bool vanishes(const void *row, int which, float x, double log_mass)
+    {
+        if (log_mass > -1000.0 || log_mass < -1023.0) return log_mass < -1000.0;
+        return ((double)x - (double)largest<TYPE>(row, which)) * c < -1000.0;
+    }
     template <int TYPE>
     __device__ float largest(const void *row, int which)
     {
@@ -804,12 +811,12 @@ __device__ __noinline__ void settle_sequence(const VerifyParams &p, SettleShared
         if (j == length) break;
         x = a.tokens[(int64_t)b * a.S + j];
         const bool inside = x >= 0 && x < a.V;
-        // u q < p, both sides times both normalisers
-        double p_x = 0, q_x = 0;
-        if (inside && zt > 0) p_x = c.weight(logit(c.t_row, x, TT), c.m[0]) * (zq > 0 ? zq : 1.0);
-        if (!a.draft) q_x = inside ? zt : 0.0;
-        else if (inside && zq > 0) q_x = c.weight(logit(c.q_row, x, QT), c.m[1]) * zt;
-        refused = !(uniform(a.u_accept[(int64_t)b * a.S + j]) * q_x < p_x);
+        // u q < p by logarithms: either may be smaller than any number of fp64
+        const float xt = inside && zt > 0 ? logit(c.t_row, x, TT) : -CUDART_INF_F, xq = a.draft && inside && zq > 0 ? logit(c.q_row, x, QT) : -CUDART_INF_F;
+        const double log_p = ((double)xt - (double)c.m[0]) * c.c - log2(zt), log_q = a.draft ? ((double)xq - (double)c.m[1]) * c.c - log2(zq) : 0.0;
+        const bool no_p = xt == -CUDART_INF_F || c.template vanishes<TT>(c.t_row, 0, xt, log_p);
+        const bool no_q = a.draft ? xq == -CUDART_INF_F || c.template vanishes<QT>(c.q_row, 1, xq, log_q) : !inside;
+        refused = no_p || !(no_q || log2(uniform(a.u_accept[(int64_t)b * a.S + j])) + log_q < log_p);
         if (refused) break;
         if (writer) out[j] = x;
     }
@@ -1109,10 +1116,15 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
                     } else if (w[0] == 0.f) {
                         how = VF_REFUSED;
                     } else if (w[0] < 1e-27f || (w[1] > 0.f && w[1] < 1e-27f)) {
-                        // entries far below their rows' largest, where weights have a floor: by their exponents, as far as fp64 has such numbers
-                        const double et = (double)xt * sc.c - (double)mt, eq = drafts && w[1] > 0.f ? (double)xq * sc.c - (double)mq : 0.0;
-                        const double by = w[1] > 0.f ? et + (double)log2f((float)zq) - eq - (double)log2f((float)(u * zt)) : 1.0;
-                        how = !(et > -900.0 && eq > -900.0 && fabs(by) > 1e-3) ? VF_UNDECIDED : by > 0 ? VF_GO_ON : VF_REFUSED;
+                        // entries far below their rows' largest, where weights have a floor: by their exponents
+                        const bool has_q = w[1] > 0.f;
+                        const double et = (double)xt * sc.c - (double)mt, eq = drafts && has_q ? (double)xq * sc.c - (double)mq : 0.0;
+                        const double by = et + (double)log2f((float)zq) - eq - (double)log2f((float)(u * zt));
+                        // (what is below 2^-1000 of its row's largest has no mass; the exponents here are relative to that rounded)
+                        if (fabs(et + 1000.0) < 1.0 || fabs(eq + 1000.0) < 1.0) how = VF_UNDECIDED;
+                        else if (et < -1000.0) how = VF_REFUSED;
+                        else if (!has_q || eq < -1000.0) how = VF_GO_ON;
+                        else how = !(fabs(by) > 1e-3) ? VF_UNDECIDED : by > 0 ? VF_GO_ON : VF_REFUSED;
                     } else {
                         how = fabs(left - right) < 2.0 * VF_EPS_P * (left + right) ? VF_UNDECIDED : left < right ? VF_GO_ON : VF_REFUSED;
                     }

@@ -188,6 +188,17 @@ def test_extreme_temperatures(T):
     agree(p)
 
 
+@pytest.mark.parametrize("T", [0.003, 0.01, 0.05, 0.2])
+@pytest.mark.parametrize("v", [6, 104, 1630, 48_003])
+def test_low_temperatures(T, v):
+    """Logits / T of some hundreds to some thousands: probabilities from one to nothing, and exponents up to the ends of fp64."""
+    for i, (target, draft) in enumerate([(BF, F32), (FH, F32), (BF, FH), (F32, None)]):
+        p = problem(300 if v < 2000 else 40, 2, v, target, draft, seed=i, noise=0.3 * (1 + i), sharp=2.0 + 6 * i, greedy_every=0)
+        p["temperature"][:] = T * (1 + torch.rand(p["temperature"].shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(i)))
+        # (rows with nearly all their mass on one entry leave residuals of down to 2^-40 in all: any decision within one is within 1e-12)
+        agree(p, allow=len(p["u_sample"]) // 5)
+
+
 def test_views_of_larger_buffers():
     b, s, v = 9, 3, 1501
     p = problem(b, s, v, BF, F32)

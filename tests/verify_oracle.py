@@ -2,6 +2,7 @@
 import numpy as np
 
 LARGEST = float(np.finfo(np.float32).max)
+LEAST = -1000 * np.log(2)        # an entry of less than 2^-1000 of its row's largest weight has none
 
 
 def masses(logits, T):
@@ -15,7 +16,8 @@ def masses(logits, T):
         one[int(np.argmax(x))] = 1.0
         return one
     with np.errstate(over="ignore"):
-        e = np.exp((x - top) / float(T))
+        at = (x - top) / float(T)
+    e = np.where(at < LEAST, 0.0, np.exp(np.maximum(at, LEAST)))
     return e / e.sum()
 
 
@@ -60,9 +62,11 @@ def verify(target, draft, tokens, u_accept, u_sample, lengths=None, temperature=
                     q[x] = 1.0
             else:
                 q = masses(draft[b, j], T)
-            left, right = uniform(u_accept[b, j]) * (q[x] if inside else 0.0), (p[x] if inside else 0.0)
-            if T > 0 and left > 0 and right > 0:
-                margin[b] = min(margin[b], abs(left - right) / max(left, right))
+            # (by logarithms: the masses may be next to the smallest numbers there are, and their product below)
+            with np.errstate(divide="ignore"):
+                left, right = np.log(uniform(u_accept[b, j])) + np.log(q[x] if inside else 0.0), np.log(p[x] if inside else 0.0)
+            if T > 0 and np.isfinite(left) and np.isfinite(right):
+                margin[b] = min(margin[b], abs(left - right))
             if not left < right:
                 refused = True
                 break
