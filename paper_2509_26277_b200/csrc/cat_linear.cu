@@ -128,16 +128,13 @@ __device__ __forceinline__ float activate(float z)
 
 // 16 tokens of this thread's output column: y = act(acc + b) + r.  `count` tokens are there.
 template <int OT, int ACT>
-__device__ __forceinline__ void finish16(const float (&acc)[16], float bias, const typename Elem<OT>::type *res, int64_t ldr,
+__device__ __forceinline__ void finish16(const float (&acc)[16], float bias, bool has, const typename Elem<OT>::type (&r)[16],
                                          typename Elem<OT>::type *out, int64_t ldy, int count)
 {
     using E = Elem<OT>;
     constexpr bool FAST = OT != CAT_F32;
     if (count >= 16) {
-        if (res) {
-            typename E::type r[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j, res += ldr) r[j] = *res;
+        if (has) {
 #pragma unroll
             for (int j = 0; j < 16; ++j, out += ldy) *out = E::down(activate<ACT, FAST>(acc[j] + bias) + E::up(r[j]));
         } else {
@@ -149,22 +146,36 @@ __device__ __forceinline__ void finish16(const float (&acc)[16], float bias, con
         for (int j = 0; j < 16; ++j)
             if (j < count) {
                 float y = activate<ACT, FAST>(acc[j] + bias);
-                if (res) y += E::up(res[j * ldr]);
+                if (has) y += E::up(r[j]);
                 out[j * ldy] = E::down(y);
             }
     }
 }
 
 template <int OT>
-__device__ __forceinline__ void finish(int act, const float (&acc)[16], float bias, const typename Elem<OT>::type *res, int64_t ldr,
+__device__ __forceinline__ void finish(int act, const float (&acc)[16], float bias, bool has, const typename Elem<OT>::type (&r)[16],
                                        typename Elem<OT>::type *out, int64_t ldy, int count)
 {
     switch (act) {
-    case CAT_ACT_RELU: finish16<OT, CAT_ACT_RELU>(acc, bias, res, ldr, out, ldy, count); break;
-    case CAT_ACT_GELU: finish16<OT, CAT_ACT_GELU>(acc, bias, res, ldr, out, ldy, count); break;
-    case CAT_ACT_GELU_TANH: finish16<OT, CAT_ACT_GELU_TANH>(acc, bias, res, ldr, out, ldy, count); break;
-    case CAT_ACT_SILU: finish16<OT, CAT_ACT_SILU>(acc, bias, res, ldr, out, ldy, count); break;
-    default: finish16<OT, CAT_ACT_NONE>(acc, bias, res, ldr, out, ldy, count); break;
+    case CAT_ACT_RELU: finish16<OT, CAT_ACT_RELU>(acc, bias, has, r, out, ldy, count); break;
+    case CAT_ACT_GELU: finish16<OT, CAT_ACT_GELU>(acc, bias, has, r, out, ldy, count); break;
+    case CAT_ACT_GELU_TANH: finish16<OT, CAT_ACT_GELU_TANH>(acc, bias, has, r, out, ldy, count); break;
+    case CAT_ACT_SILU: finish16<OT, CAT_ACT_SILU>(acc, bias, has, r, out, ldy, count); break;
+    default: finish16<OT, CAT_ACT_NONE>(acc, bias, has, r, out, ldy, count); break;
+    }
+}
+
+// the residual's entries for them
+template <typename T>
+__device__ __forceinline__ void load16(T (&r)[16], const T *from, int64_t ld, int64_t count)
+{
+    if (count >= 16) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j, from += ld) r[j] = *from;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (j < count) r[j] = from[j * ld];
     }
 }
 
@@ -369,56 +380,84 @@ linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ 
             const bool inside = n < p.N;
             const int64_t t0 = (int64_t)tt * p.nt;
             const float bias = p.bias && inside && p.splits == 1 ? load_as_float(p.bias, n, p.bias_type) : 0.f;
-            float sum[OT == CAT_F32 ? 4 : 1][16];     // (fp32 results: the runs so far)
-            for (int first = slab0; first < slab1; first += run, ++ti) {
-                const int b = ti & 1;
-                const bool whole = first + run >= slab1;       // the last run
-                ok = mbar_wait_warp(smem_u32(&sh.tmem_full[b]), (ti >> 1) & 1u, abort_flag, p.ctl);
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * p.nt);
-                uint32_t raw16[16];
-                if (OT == CAT_F32 && run < slab1 - slab0) {
-                    // runs are added up in registers; the last one's accumulator takes the whole, so that one loop finishes either kind
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int c = ((warps - 2) / 4 * i + part) * 16;
-                        if (c >= p.nt) break;
-                        tmem_ld16_issue(taddr + (uint32_t)c, raw16);
-                        tmem_ld_wait16(raw16);
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) sum[OT == CAT_F32 ? i : 0][j] = __uint_as_float(raw16[j]) + (first > slab0 ? sum[OT == CAT_F32 ? i : 0][j] : 0.f);
-                        if (whole) tmem_st16(taddr + (uint32_t)c, sum[OT == CAT_F32 ? i : 0]);
-                    }
-                    if (whole) tmem_st_wait();
-                }
-#pragma unroll 1
-                for (int c = part * 16; whole && c < p.nt; c += (warps - 2) * 4) {
-                    tmem_ld16_issue(taddr + (uint32_t)c, raw16);
-                    tmem_ld_wait16(raw16);
-                    float acc[16];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) acc[j] = __uint_as_float(raw16[j]);
-                    if (p.splits > 1) {
-                        // [token][output column] of this CTA's part, in the ring (every slab has been consumed)
-                        float *to = reinterpret_cast<float *>(ring_ptr) + (size_t)c * 128 + quarter * 32 + lane;
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) to[j * 128] = acc[j];
-                    } else if (inside && t0 + c < p.M) {
-                        const int64_t row = t0 + c;
-                        const int count = (int)min((int64_t)16, p.M - row);
-                        const T *res = p.residual ? reinterpret_cast<const T *>(p.residual) + row * p.ldr + n : nullptr;
-                        finish<OT>(p.act, acc, bias, res, p.ldr, reinterpret_cast<T *>(p.Y) + row * p.ldy + n, p.ldy, count);
-                    }
-                }
-                // accumulator buffer b may be overwritten from here on
+            // 16-bit results: the residual of a chunk is on its way while the accumulator, or the chunk before, is waited for
+            constexpr bool AHEAD = OT != CAT_F32;
+            const bool has = p.residual && inside && p.splits == 1;
+            T ahead[16];
+            auto fetch = [&](T (&r)[16], int c) {
+                if (has && c < p.nt && t0 + c < p.M)
+                    load16<T>(r, reinterpret_cast<const T *>(p.residual) + (t0 + c) * p.ldr + n, p.ldr, p.M - t0 - c);
+            };
+            // accumulator buffer b may be overwritten from here on
+            auto release = [&](int b) {
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {
                     if (PAIR) mbar_arrive_cluster(mapa_cluster(smem_u32(&sh.tmem_empty[b]), leader));
                     else mbar_arrive(smem_u32(&sh.tmem_empty[b]));
                 }
+            };
+            auto accumulator = [&](int b) { return tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * p.nt); };
+            if (AHEAD) fetch(ahead, part * 16);
+            uint32_t raw16[16];
+            if (OT == CAT_F32 && runs > 1) {
+                // runs are added up in registers; the last one's accumulator takes the whole, so that one loop finishes either kind
+                float sum[4][16];
+                for (int i = 0; i < runs; ++i, ++ti) {
+                    const int b = ti & 1;
+                    ok = mbar_wait_warp(smem_u32(&sh.tmem_full[b]), (ti >> 1) & 1u, abort_flag, p.ctl);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int c = ((warps - 2) / 4 * k + part) * 16;
+                        if (c >= p.nt) break;
+                        tmem_ld16_issue(accumulator(b) + (uint32_t)c, raw16);
+                        tmem_ld_wait16(raw16);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) sum[k][j] = i > 0 ? sum[k][j] + __uint_as_float(raw16[j]) : __uint_as_float(raw16[j]);
+                        if (i == runs - 1) tmem_st16(accumulator(b) + (uint32_t)c, sum[k]);
+                    }
+                    if (i == runs - 1) {
+                        tmem_st_wait();
+                        break;
+                    }
+                    release(b);
+                }
+            } else {
+                ok = mbar_wait_warp(smem_u32(&sh.tmem_full[ti & 1]), (ti >> 1) & 1u, abort_flag, p.ctl);
+                tc_fence_after();
             }
+            if (!ok) break;
+            const int b = ti & 1;
+#pragma unroll 1
+            for (int c = part * 16; c < p.nt; c += (warps - 2) * 4) {
+                tmem_ld16_issue(accumulator(b) + (uint32_t)c, raw16);
+                tmem_ld_wait16(raw16);
+                float acc[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[j] = __uint_as_float(raw16[j]);
+                if (p.splits > 1) {
+                    // [token][output column] of this CTA's part, in the ring (every slab has been consumed)
+                    float *to = reinterpret_cast<float *>(ring_ptr) + (size_t)c * 128 + quarter * 32 + lane;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) to[j * 128] = acc[j];
+                } else if (inside && t0 + c < p.M) {
+                    const int64_t row = t0 + c;
+                    const int count = (int)min((int64_t)16, p.M - row);
+                    T r[16];
+                    if (AHEAD) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) r[j] = ahead[j];
+                        fetch(ahead, c + (warps - 2) * 4);
+                    } else {
+                        fetch(r, c);
+                    }
+                    finish<OT>(p.act, acc, bias, has, r, reinterpret_cast<T *>(p.Y) + row * p.ldy + n, p.ldy, count);
+                }
+            }
+            release(b);
+            ++ti;
         }
     }
 
