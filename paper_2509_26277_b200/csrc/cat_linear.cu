@@ -463,6 +463,13 @@ linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ 
 
     tc_fence_before();
     __syncthreads();
+    if (!PAIR && warp == 1) {
+        // Given back before this CTA waits for the others of its cluster: a CTA of theirs may be waiting for TMEM that another stream's kernel
+        // holds, which in turn waits for this SM's.  (Pairs have their SMs to themselves: their rings leave no other kernel with TMEM room.)
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc(tmem_base, (uint32_t)p.tmem_cols);
+    }
     if (p.splits > 1) {
         // The parts meet: split q of the cluster finishes every q-th token of the tile, the parts in order.  A warp takes a token, a lane four of its
         // 128 output columns.
@@ -501,11 +508,10 @@ linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ 
             }
     }
     if (PAIR || p.splits > 1) cluster_sync();   // no CTA's shared memory or TMEM goes away under another
-    if (warp == 1) {
+    if (PAIR && warp == 1) {
         __syncwarp();
         tc_fence_after();
-        if (PAIR) tmem_dealloc_pair(tmem_base, (uint32_t)p.tmem_cols);
-        else tmem_dealloc(tmem_base, (uint32_t)p.tmem_cols);
+        tmem_dealloc_pair(tmem_base, (uint32_t)p.tmem_cols);
     }
 }
 

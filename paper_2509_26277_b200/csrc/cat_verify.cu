@@ -6,11 +6,15 @@
 // the sums.  The library's way with such decisions: fast fp32 weights whose errors are bounded, and an fp64 pass for what is closer
 // than the bound.
 //
-// verify_kernel.  A cluster of 1 to 16 CTAs takes a sequence, every CTA a contiguous part of the vocabulary, every warp chunks of 32 or 128
+// verify_kernel.  A cluster of 1 to 8 CTAs takes a sequence, every CTA a contiguous part of the vocabulary, every warp chunks of 32 or 128
 // 16-byte granules (one or four per lane, in flight together).  A chunk leaves its largest exponent (an integer in units of log 2) and its
 // sum of weights, so one read of a row gives its normaliser and, where the row itself is drawn from, the chunk that holds the token; only a
-// residual reads its two rows again, out of L2.  `group` rows and their drafts go through between two exchanges: one where reading the rows
-// behind a refusal for nothing costs more than an exchange, up to eight where it does not.
+// residual reads its two rows again, out of L2.  `group` rows and their drafts go through between two exchanges: few where reading the rows
+// behind a refusal for nothing costs more than an exchange, up to eight where it does not.  What bounds it: a small batch the chain of load,
+// sums, exchange, decision and draw (8 sequences of 4 drafts over 32 000: 15 us, the bytes 2.8); a large one the instructions, about twelve an entry
+// (256 rows of 50 001: 17 us, 1.5 TB/s; 64 sequences of 7 drafts over 128 000: 70 us for the 130 MB that it reads).
+//
+// verify_settle_kernel, and the same in verify_kernel: what the sums leave undecided, in fp64.  Bound by latency: 12 us a sequence of 32 000.
 //
 // A weight 2^(x c - M), c = log2(e) / T, M an integer: n = rint(x c), f = x c - n in two fused steps on c as a sum of two floats, 2^f
 // from the special function unit, n - M added to the exponent.  Its relative error does not grow with |x c|: f is off by at most
@@ -22,12 +26,11 @@
 #include <cuda_fp16.h>
 #include <math_constants.h>
 
-
 namespace cat {
 namespace {
 
 constexpr int VF_THREADS = 512;
-constexpr int VF_MAX_CLUSTER = 16;
+constexpr int VF_SETTLE_CLUSTER = 16;                      // (largest cluster there is)
 constexpr double VF_NO_RESIDUAL = 9.094947017729282e-13;   // 2^-40: a residual of less mass is what rounding left of none
 
 __device__ __forceinline__ uint32_t cta_rank()
@@ -66,7 +69,7 @@ __device__ __forceinline__ int peer_s32(const int *p, uint32_t rank)
     return v;
 }
 
-// A logit as the definitions take it: NaN counts as -inf, +inf as the largest number. 
+// A logit as the definitions take it: NaN counts as -inf, +inf as the largest number.
 __device__ __forceinline__ float clean(float x)
 {
     const uint32_t u = __float_as_uint(x), size = u & 0x7fffffffu;
@@ -1307,8 +1310,8 @@ cudaError_t launch_verify(const VerifyArgs &a, void *workspace, cudaStream_t s)
     p.group = (int)((((int64_t)40 << 20) + pair_bytes - 1) / pair_bytes);
     if (p.group > p.max_group) p.group = p.max_group;
     p.slots = p.max_group * (per_t + per_q);
-    // An undecided sequence is settled by the CTAs that have it where four passes over a row do; else by a cluster of 16 in a launch of its own
-    // (64 sequences, V = 128 000: 116 us against 142; 256 sequences, V = 50 001: 39 us against 88).
+    // An undecided sequence is settled by the CTAs that have it where every thread has sixteen entries of a row at most; else by a cluster of 16 in a
+    // launch of its own (64 sequences, V = 128 000: 116 us against 142; 256 sequences, V = 50 001: 39 us against 88).
     p.settle = entries <= (int64_t)16 * VF_THREADS * p.size;
     // (the weights of two rows in fp64: where a CTA has an SM to itself, or they are small)
     auto kept_bytes = [&](int size) { return ((entries + 6) / 4 / size + 1) * 64; };
@@ -1340,7 +1343,7 @@ cudaError_t launch_verify(const VerifyArgs &a, void *workspace, cudaStream_t s)
     count_launch();
     if (e != cudaSuccess || p.settle) return e;
 
-    p.size = VF_MAX_CLUSTER;
+    p.size = VF_SETTLE_CLUSTER;
     p.keep = kept_bytes(p.size) <= 200 * 1024;
     const int clusters = a.B < sms / p.size ? a.B : sms / p.size;
     cfg.gridDim = dim3((unsigned)(clusters * p.size), 1, 1);
