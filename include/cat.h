@@ -358,7 +358,8 @@ cat_status_t cat_apply_pca(const float *Yq, int64_t N, int32_t D, int32_t K, int
  * layer before it:
  *   Y[i,:] = act(X[i,:] W^T + bias) + residual[i,:]            (i < M; W is [N, K], row n the weights of output column n)
  * X [M, K] and W [N, K] are of in_type, CAT_BF16 or CAT_F16; Y [M, N] and residual [M, N] of out_type (any of the three);
- * bias [N] of bias_type, may be NULL; residual may be NULL, or Y itself (with ldr = ldy; no other overlap).
+ * bias [N] of bias_type, may be NULL; residual may be NULL, or Y itself (with ldr = ldy).  Y shares no other memory with what is read (it may be
+ * other columns of the same buffer, with rows as many bytes apart).
  * Rows are ldx, ldw, ldr, ldy elements apart (at least K, K, N, N; with one row its distance is not looked at); no base
  * address needs more alignment than its element.  Products and sums are formed in fp32 on the tensor cores, bias, activation and residual in
  * fp32 behind them, and the result is rounded once to out_type (overflow of fp16 gives infinities).  Non-finite inputs
@@ -403,7 +404,7 @@ cat_status_t cat_linear(const void *X, int64_t ldx, const void *W, int64_t ldw, 
  * nothing and gives token -1.  A residual of less mass than 2^-40 is what rounding left of none: the draw is from p_j then.
  * The outputs are those of fp64 arithmetic: what fast fp32 sums cannot decide within their error bound goes to an fp64 pass
  * (cat_workspace_report counts those sequences).  S = 0 is allowed (draft, draft_tokens and u_accept may be NULL then), B = 0 does nothing.
- * The outputs overlap neither each other nor an input.
+ * The outputs overlap neither each other nor an input, and lie nowhere between the first and the last of the target's, or the draft's, logits.
  * Limits: B <= CAT_VERIFY_MAX_B, S <= CAT_VERIFY_MAX_S, V <= CAT_VERIFY_MAX_V.  Workspace: CAT_VERIFY_WORKSPACE_BYTES.
  */
 #define CAT_VERIFY_MAX_B (1 << 20)

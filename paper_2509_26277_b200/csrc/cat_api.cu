@@ -844,6 +844,18 @@ static bool overlap(const void *a, size_t n, const void *b, size_t m)
     return p && q && p < q + m && q < p + n;
 }
 
+// Do two matrices share a byte?  (Rows of `width` bytes, `pitch` apart.)  Of equal distances the columns tell; of others what lies between the first
+// and the last byte counts as the matrix's.
+static bool rows_meet(const void *a, int64_t rows_a, int64_t width_a, int64_t pitch_a, const void *b, int64_t rows_b, int64_t width_b, int64_t pitch_b)
+{
+    const __int128 p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+    if (!a || !b || p >= q + (__int128)(rows_b - 1) * pitch_b + width_b || q >= p + (__int128)(rows_a - 1) * pitch_a + width_a) return false;
+    const int64_t pitch = rows_a > 1 ? pitch_a : pitch_b;
+    if ((rows_a > 1 && rows_b > 1 && pitch_a != pitch_b) || (rows_a == 1 && rows_b == 1) || width_a > pitch || width_b > pitch) return true;
+    const int64_t d = (int64_t)(((q - p) % pitch + pitch) % pitch);   // b's first column, from a's
+    return d < width_a || d + width_b > pitch;
+}
+
 // (the distance of the only row of a matrix says nothing)
 static int64_t row_distance(int64_t ld, int64_t rows, int32_t K) { return rows > 1 ? ld : ((int64_t)K + 7) & ~(int64_t)7; }
 
@@ -878,6 +890,11 @@ cat_status_t cat_linear(const void *X, int64_t ldx, const void *W, int64_t ldw, 
         return CAT_ERR_ALIGN;
     LinearArgs a{X, W, bias, residual, Y, row_distance(ldx, M, K), row_distance(ldw, N, K), ldr, ldy, M, N, K, in_type, bias_type, out_type, activation};
     if (!workspace || !aligned16(workspace) || workspace_bytes < linear_workspace_bytes(X, a.ldx, W, a.ldw, M, N, K)) return CAT_ERR_WORKSPACE;
+    const int64_t in = 2, out = out_type == CAT_F32 ? 4 : 2, wide = (int64_t)N * out;
+    if (rows_meet(Y, M, wide, ldy * out, X, M, K * in, a.ldx * in) || rows_meet(Y, M, wide, ldy * out, W, N, K * in, a.ldw * in) ||
+        (residual != Y && rows_meet(Y, M, wide, ldy * out, residual, M, wide, ldr * out)) ||
+        rows_meet(Y, M, wide, ldy * out, bias, 1, N * (bias_type == CAT_F32 ? 4 : 2), 0))
+        return CAT_ERR_SHAPE;
     CAT_CUDA(launch_linear(a, workspace, reinterpret_cast<cudaStream_t>(stream)));
     return CAT_OK;
 }
@@ -907,6 +924,18 @@ cat_status_t cat_verify_drafts(const void *target, int32_t target_type, int64_t 
         for (const auto &i : in)
             if (overlap(o.at, o.bytes, i.at, i.bytes)) return CAT_ERR_SHAPE;
     if (overlap(out[0].at, out[0].bytes, out[1].at, out[1].bytes)) return CAT_ERR_SHAPE;
+    // (likewise the logits: what lies between their first and last byte)
+    auto among = [&](const void *logits, int32_t type, int64_t rows, int64_t seq, int64_t row) {
+        const __int128 at = reinterpret_cast<uintptr_t>(logits), size = type == CAT_F32 ? 4 : 2;
+        const __int128 end = at + ((B > 1 ? (__int128)(B - 1) * seq : 0) + (rows > 1 ? (__int128)(rows - 1) * row : 0) + V) * size;
+        for (const auto &o : out) {
+            const __int128 from = reinterpret_cast<uintptr_t>(o.at);
+            if (from < end && at < from + (__int128)o.bytes) return true;
+        }
+        return false;
+    };
+    if (among(target, target_type, S + 1, target_seq, target_row) || (draft && S > 0 && among(draft, draft_type, S, draft_seq, draft_row)))
+        return CAT_ERR_SHAPE;
     if (!workspace || !aligned16(workspace) || workspace_bytes < CAT_VERIFY_WORKSPACE_BYTES) return CAT_ERR_WORKSPACE;
     const VerifyArgs a{target, S > 0 ? draft : nullptr, draft_tokens, draft_lengths, temperature, u_accept, u_sample, tokens_out, accepted_out,
                        target_seq, target_row, draft_seq, draft_row, target_type, draft_type, B, S, V};

@@ -200,3 +200,29 @@ def test_refusals_on_the_device():
     with pytest.raises(B.CatError) as e:
         B.cat_linear(X, W, out=torch.zeros((1, 40), device="cuda", dtype=BF).expand(8, 40))   # one row for all
     assert e.value.status == 2
+
+
+@pytest.mark.parametrize("m", [1, 5, 300])
+def test_columns_of_one_buffer(m):
+    """X, the result and the weights' rows side by side in one buffer share no memory; a shifted residual and the result itself do."""
+    for first, second in [(0, 128), (136, 0)]:
+        buffer = torch.full((m + 1, 300), 7.0, dtype=BF, device="cuda")
+        X, W, _ = data(m, 136, 120, BF)
+        x, y = buffer[:m, first:first + 120], buffer[1:, second:second + 136]
+        x.copy_(X)
+        B.cat_linear(x, W, out=y)
+        check(X, W, None, None, "none", BF, y)
+        assert torch.equal(x, X) and bool((buffer[1:, 264:] == 7.0).all())
+    X, W, _ = data(m, 120, 120, BF)
+    for kwargs in [dict(out=X), dict(out=W[:m] if m <= 120 else X), dict(out=buffer[:m, :120], residual=buffer[:m, 8:128])]:
+        with pytest.raises(B.CatError) as e:
+            B.cat_linear(X, W, **kwargs)
+        assert e.value.status == 2
+
+
+# the largest number of rows, of columns, and the longest inner dimension
+@pytest.mark.parametrize("m,n,k", [(1 << 24, 1, 8), (1 << 24, 2, 3), (1, 1 << 20, 8), (3, 1 << 20, 5), (2, 3, 1 << 20), (150, 5, (1 << 20) - 1)])
+@pytest.mark.parametrize("out_dtype", [BF, F32])
+def test_the_largest_sizes(m, n, k, out_dtype):
+    X, W, _ = data(m, n, k, BF)
+    check(X, W, None, None, "none", out_dtype, B.cat_linear(X, W, out_dtype=out_dtype))

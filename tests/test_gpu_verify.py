@@ -295,3 +295,39 @@ def test_refusals_on_the_device():
     with pytest.raises(B.CatError) as e:
         B.cat_verify_drafts(**dict(p, target=p["target"][:, :1].expand(4, 3, 100)))   # one row for all
     assert e.value.status == 2
+
+
+@pytest.mark.parametrize("b,s,v", [(2, 256, 600), (1, 256, 33_000), (1, 0, 1 << 22)])
+def test_the_most_drafts_and_the_largest_vocabulary(b, s, v):
+    p = problem(b, s, v, FH, BF, noise=0.02)
+    p["draft_lengths"] = None
+    agree(p)
+
+
+@pytest.mark.parametrize("v", [1, 7, 40])
+def test_the_largest_batch(v):
+    """2^20 sequences, every third of them greedy, against whole-batch arithmetic in 64 bits."""
+    b = 1 << 20
+    g = torch.Generator(device="cuda").manual_seed(v)
+    t = torch.randn((b, 1, v), generator=g, device="cuda").to(BF)
+    T = torch.ones((b,), device="cuda")
+    T[::3] = 0
+    u = torch.rand((b,), generator=g, device="cuda")
+    none = torch.empty((b, 0), device="cuda")
+    tokens, kept = B.cat_verify_drafts(t, None, none.int(), none, u, temperature=T)
+    mass = torch.exp(t[:, 0].double() - t[:, 0].double().amax(1, keepdim=True))
+    total = mass.cumsum(1)
+    drawn = (total > u.double()[:, None] * total[:, -1:]).int().argmax(1)
+    largest = t[:, 0] == t[:, 0].amax(1, keepdim=True)
+    want = torch.where(T > 0, drawn, largest.int().argmax(1))
+    close = (T > 0) & ((total - u.double()[:, None] * total[:, -1:]).abs().amin(1) < 1e-11)
+    same = tokens[:, 0] == want
+    assert bool((same | close).all()) and int(close.sum()) <= 1 and not bool(kept.any())
+
+
+def test_outputs_among_the_logits_are_refused():
+    p = problem(1, 1, 100, BF, F32)
+    for kwargs in [dict(tokens_out=p["draft"].view(torch.int32)[0, :, :2]), dict(accepted_out=p["target"].view(torch.int32)[0, 1, 49:])]:
+        with pytest.raises(B.CatError) as e:
+            B.cat_verify_drafts(**p, **kwargs)
+        assert e.value.status == 2

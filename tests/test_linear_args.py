@@ -53,3 +53,11 @@ def test_binding_refuses_cpu_tensors():
     with pytest.raises(TypeError):
         B.cat_linear(x, x)
     assert ctypes.sizeof(ctypes.c_void_p) == 8
+
+
+@pytest.mark.parametrize("over", [dict(Y=AT), dict(X=AT + 65536, Y=AT), dict(X=AT + 65536, Y=AT + 8 * 16 * 4 - 4, bias=AT + 65536 * 2, W=AT + 8 * 16 * 4),
+                                  dict(X=AT + 65536, W=AT + 131072, bias=AT + 4, Y=AT), dict(X=AT + 65536, W=AT + 131072, residual=AT + 64, ldr=16, Y=AT),
+                                  dict(X=AT, ldx=128, Y=AT + 124, ldy=64), dict(X=AT + 128, ldx=128, W=AT + 65536, Y=AT + 192, ldy=64),
+                                  dict(X=AT, ldx=128, W=AT + 65536, Y=AT + 256 * 7 + 64, ldy=100), dict(M=1, X=AT + 65536, W=AT + 128, Y=AT + 124, ldy=1)])
+def test_results_among_what_is_read_are_refused(over):
+    assert call(**over) == 2

@@ -75,3 +75,15 @@ def test_oracle_masks_greedy_and_rows_without_mass():
     assert out.tolist() == [[0, -1, -1]] and kept[0] == 0
     assert O.masses([inf, 1.0, inf], 1.0).tolist() == [0.5, 0.0, 0.5]
     assert O.masses([-3.4e38, -3.4e38], 1.0).tolist() == [0.5, 0.5]
+
+
+@pytest.mark.parametrize("over", [dict(out=AT), dict(kept=AT + 1996), dict(draft=AT + 16384, out=AT + 16384 + 3196), dict(draft=AT + 16384, kept=AT + 16384),
+                                  dict(target=AT + 4096 - 1996), dict(ts=1 << 61, target=AT + 65536, out=AT + 131072)])
+def test_outputs_among_the_logits_are_refused(over):
+    """The first and the last of 2 x (5 rows of 100 bf16) and 2 x (4 rows of 100 fp32); distances whose bytes pass 64 bits."""
+    assert call(**over) == 2
+
+
+def test_outputs_next_to_the_logits_are_not():
+    assert call(out=AT + 3200, kept=AT + 3240, ws=None) == 4
+    assert call(target=AT + 4096 + 40, ws=None) == 4
