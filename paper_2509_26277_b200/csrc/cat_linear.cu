@@ -199,6 +199,14 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const float (&v)[16])
         "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
         : "memory");
 }
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float (&v)[8])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+        : "r"(taddr)
+        : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // arrives on the barrier at this shared-memory offset in both CTAs of the pair whose first one has this rank
@@ -257,8 +265,8 @@ linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ 
 
     // Sums of fp32 results run over at most LN_RUN slabs at a time: the tensor cores truncate an accumulator at every step, always towards zero, and
     // what that costs grows with the length of the run.  The epilogue adds the runs up in registers, rounding to nearest.  Relative error at 2048
-    // inner columns (2-norm; fp32 sums in another order: 3.7e-7), time of 50 000 x 1000: one run 1.9e-6, 150 us; 16 slabs 9.1e-7, 166 us; 12 slabs
-    // 6.1e-7, 174 us; 8 slabs 4.3e-7, 181 us (the epilogue of a tile's last run no longer passes under the next one).
+    // inner columns (2-norm; fp32 sums in another order: 3.7e-7), time of 50 000 x 1000 under the power cap: one run 1.9e-6, 192 us; 16 slabs 9.1e-7,
+    // 194 us; 12 slabs 6.1e-7, 196 us; 8 slabs 4.3e-7, 201 us.
     const int in_split = slab1 - slab0, runs = OT == CAT_F32 ? (in_split + LN_RUN - 1) / LN_RUN : 1, run = (in_split + runs - 1) / runs;
 
     if (tid == 0) {
@@ -401,9 +409,15 @@ linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ 
             if (AHEAD) fetch(ahead, part * 16);
             uint32_t raw16[16];
             if (OT == CAT_F32 && runs > 1) {
-                // runs are added up in registers; the last one's accumulator takes the whole, so that one loop finishes either kind
+                // Runs are added up in registers, eight columns at a time: the sums take 64 of 96, and with sixteen at a time the loop spills (50 000 x 1000
+                // x 2048: 211 us against 198).
                 float sum[4][16];
-                for (int i = 0; i < runs; ++i, ++ti) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[k][j] = 0.f;
+#pragma unroll 1
+                for (int left = runs;; ++ti) {
                     const int b = ti & 1;
                     ok = mbar_wait_warp(smem_u32(&sh.tmem_full[b]), (ti >> 1) & 1u, abort_flag, p.ctl);
                     if (!ok) break;
@@ -411,18 +425,51 @@ linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ 
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int c = ((warps - 2) / 4 * k + part) * 16;
-                        if (c >= p.nt) break;
-                        tmem_ld16_issue(accumulator(b) + (uint32_t)c, raw16);
-                        tmem_ld_wait16(raw16);
+                        if (c < p.nt) {
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) sum[k][j] = i > 0 ? sum[k][j] + __uint_as_float(raw16[j]) : __uint_as_float(raw16[j]);
-                        if (i == runs - 1) tmem_st16(accumulator(b) + (uint32_t)c, sum[k]);
+                            for (int h = 0; h < 16; h += 8) {
+                                float v[8];
+                                tmem_ld8(accumulator(b) + (uint32_t)(c + h), v);
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) sum[k][h + j] += v[j];
+                            }
+                        }
                     }
-                    if (i == runs - 1) {
-                        tmem_st_wait();
-                        break;
-                    }
+                    if (--left == 0) break;
                     release(b);
+                }
+                if (ok && p.splits == 1 && !p.residual && p.act == CAT_ACT_NONE) {
+                    // Nothing but the bias follows: out of the registers, the accumulator free before that (192 us; more work here would spill again).
+                    release(ti & 1);
+                    ++ti;
+                    if (inside) {
+                        T *out = reinterpret_cast<T *>(p.Y) + (t0 + part * 16) * p.ldy + n;
+                        const int rest = (int)min((int64_t)p.nt, p.M - t0) - part * 16;
+                        const int64_t step = (int64_t)(warps - 2) * 4 * p.ldy;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k, out += step) {
+                            const int count = rest - (warps - 2) * 4 * k;
+                            T *o = out;
+                            if (count >= 16) {
+#pragma unroll
+                                for (int j = 0; j < 16; ++j, o += p.ldy) *o = E::down(sum[k][j] + bias);
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 16; ++j, o += p.ldy)
+                                    if (j < count) *o = E::down(sum[k][j] + bias);
+                            }
+                        }
+                    }
+                    continue;
+                }
+                // The last run's accumulator takes the sums, and one loop finishes either kind.
+                if (ok) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int c = ((warps - 2) / 4 * k + part) * 16;
+                        if (c < p.nt) tmem_st16(accumulator(ti & 1) + (uint32_t)c, sum[k]);
+                    }
+                    tmem_st_wait();
                 }
             } else {
                 ok = mbar_wait_warp(smem_u32(&sh.tmem_full[ti & 1]), (ti >> 1) & 1u, abort_flag, p.ctl);
