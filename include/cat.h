@@ -361,8 +361,10 @@ cat_status_t cat_apply_pca(const float *Yq, int64_t N, int32_t D, int32_t K, int
  * bias [N] of bias_type, may be NULL; residual may be NULL, or Y itself (with ldr = ldy).  Y shares no other memory with what is read (it may be
  * other columns of the same buffer, with rows as many bytes apart).
  * Rows are ldx, ldw, ldr, ldy elements apart (at least K, K, N, N; with one row its distance is not looked at); no base
- * address needs more alignment than its element.  Products and sums are formed in fp32 on the tensor cores, bias, activation and residual in
- * fp32 behind them, and the result is rounded once to out_type (overflow of fp16 gives infinities).  Non-finite inputs
+ * address needs more alignment than its element.  Products are exact and sums formed in fp32 on the tensor cores, which truncate a sum
+ * at every 16 inner columns where other fp32 sums round it (at most 768 columns, for a 16-bit out_type 1536, are added so before the next ones
+ * are, rounded to nearest); bias, activation and residual in fp32 behind them, and the result is rounded once to out_type (overflow of fp16 gives
+ * infinities).  Non-finite inputs
  * propagate as the arithmetic has it.  Activations:
  *   CAT_ACT_RELU       max(z, 0)                     CAT_ACT_GELU       z Phi(z) (erf form)
  *   CAT_ACT_GELU_TANH  z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2          CAT_ACT_SILU  z / (1 + e^-z)

@@ -24,7 +24,8 @@ constexpr int LN_BK = 64;                       // inner columns per slab (128 b
 constexpr int LN_MAX_STAGES = 12;
 constexpr int LN_EPI_WARPS = 16;                // warps of the epilogue at most: four per quarter of the TMEM lanes
 constexpr int LN_MAX_THREADS = 32 * (2 + LN_EPI_WARPS);
-constexpr int LN_RUN = 12;                      // slabs per run of an accumulator at most, where the result is fp32 (see linear_kernel)
+constexpr int LN_RUN = 12;                      // slabs per run of an accumulator at most, where the result is fp32 (see linear_kernel) ...
+constexpr int LN_RUN_16 = 24;                   // ... and where it is rounded to 16 bits
 constexpr int LN_GROUP = 8;                     // token tiles that share a sweep over the weights
 
 struct LinearParams {
@@ -237,7 +238,9 @@ __device__ __forceinline__ void tile_of(const LinearParams &p, int unit, int &tw
     tt = g * LN_GROUP + rem - tw * gs;
 }
 
-template <bool PAIR, int OT>
+// RUNS: a 16-bit result's accumulator may take several runs.  (With one the epilogue has the registers to itself: 4999 x 2047 x 1001 38 us, 40 with
+// the code for several.)
+template <bool PAIR, int OT, bool RUNS>
 __global__ void __launch_bounds__(LN_MAX_THREADS, 1)
 linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapX, const __grid_constant__ LinearParams p)
 {
@@ -263,11 +266,15 @@ linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ 
     const int slabs = (p.K + LN_BK - 1) / LN_BK;
     const int slab0 = (int)((int64_t)slabs * split / p.splits), slab1 = (int)((int64_t)slabs * (split + 1) / p.splits);
 
-    // Sums of fp32 results run over at most LN_RUN slabs at a time: the tensor cores truncate an accumulator at every step, always towards zero, and
-    // what that costs grows with the length of the run.  The epilogue adds the runs up in registers, rounding to nearest.  Relative error at 2048
-    // inner columns (2-norm; fp32 sums in another order: 3.7e-7), time of 50 000 x 1000 under the power cap: one run 1.9e-6, 192 us; 16 slabs 9.1e-7,
-    // 194 us; 12 slabs 6.1e-7, 196 us; 8 slabs 4.3e-7, 201 us.
-    const int in_split = slab1 - slab0, runs = OT == CAT_F32 ? (in_split + LN_RUN - 1) / LN_RUN : 1, run = (in_split + runs - 1) / runs;
+    // An accumulator runs over at most LN_RUN (LN_RUN_16) slabs at a time: the tensor cores truncate it at every step, always towards zero, and
+    // what that costs grows with the length of the run.  The epilogue adds the runs up in registers, rounding to nearest.
+    // fp32 results: relative error at 2048 inner columns (2-norm; fp32 sums in another order: 3.7e-7), time of 50 000 x 1000 under the power cap: one
+    // run 1.9e-6, 192 us; 16 slabs 9.1e-7, 194 us; 12 slabs 6.1e-7, 196 us; 8 slabs 4.3e-7, 201 us.
+    // 16-bit results: how far they are from those of fp32 sums in another order (2-norm; numbers that round to the other neighbour) at 8192 and at 4096
+    // inner columns, time of 16384 x 16384 x 4096 under the power cap: one run 1.7e-4 and 1.5e-4, 1736 us; 32 slabs 8e-5 and 1.0e-4, 1753 us; 24 slabs 7e-5 and
+    // 8e-5, 1779 us; 16 slabs 6e-5 and 7e-5, 1801 us.
+    const int in_split = slab1 - slab0, longest = OT == CAT_F32 ? LN_RUN : LN_RUN_16;
+    const int runs = RUNS ? (in_split + longest - 1) / longest : 1, run = (in_split + runs - 1) / runs;
 
     if (tid == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mapW)) : "memory");
@@ -406,9 +413,9 @@ linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ 
                 }
             };
             auto accumulator = [&](int b) { return tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * p.nt); };
-            if (AHEAD) fetch(ahead, part * 16);
+            if (AHEAD && runs == 1) fetch(ahead, part * 16);
             uint32_t raw16[16];
-            if (OT == CAT_F32 && runs > 1) {
+            if (RUNS && runs > 1) {
                 // Runs are added up in registers, eight columns at a time: the sums take 64 of 96, and with sixteen at a time the loop spills (50 000 x 1000
                 // x 2048: 211 us against 198).
                 float sum[4][16];
@@ -438,7 +445,7 @@ linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ 
                     if (--left == 0) break;
                     release(b);
                 }
-                if (ok && p.splits == 1 && !p.residual && p.act == CAT_ACT_NONE) {
+                if (OT == CAT_F32 && ok && p.splits == 1 && !p.residual && p.act == CAT_ACT_NONE) {
                     // Nothing but the bias follows: out of the registers, the accumulator free before that (192 us; more work here would spill again).
                     release(ti & 1);
                     ++ti;
@@ -471,6 +478,7 @@ linear_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ 
                     }
                     tmem_st_wait();
                 }
+                if (AHEAD) fetch(ahead, part * 16);
             } else {
                 ok = mbar_wait_warp(smem_u32(&sh.tmem_full[ti & 1]), (ti >> 1) & 1u, abort_flag, p.ctl);
                 tc_fence_after();
@@ -740,9 +748,9 @@ cudaError_t launch_linear(const LinearArgs &a, void *workspace, cudaStream_t s)
     int dev = 0;
     if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
     const uint64_t dev_bit = dev < 64 ? (uint64_t)1 << dev : 0;
-#define CAT_LINEAR_LAUNCH(PAIR, OT)                                                                                             \
+#define CAT_LINEAR_LAUNCH(PAIR, OT, RUNS)                                                                                       \
     do {                                                                                                                        \
-        auto kern = linear_kernel<PAIR, OT>;                                                                                    \
+        auto kern = linear_kernel<PAIR, OT, RUNS>;                                                                              \
         static std::atomic<uint64_t> ready{0};      /* (a bit per device: the attribute is set once) */                           \
         if (!(dev_bit & ready.load(std::memory_order_relaxed))) {                                                                \
             if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024)) != cudaSuccess) return e; \
@@ -750,14 +758,19 @@ cudaError_t launch_linear(const LinearArgs &a, void *workspace, cudaStream_t s)
         }                                                                                                                        \
         e = cudaLaunchKernelEx(&cfg, kern, mapW, mapX, p);                                                                      \
     } while (0)
+    const bool several = ((a.K + LN_BK - 1) / LN_BK + pl.splits - 1) / pl.splits > LN_RUN_16;
     if (pl.pair) {
-        if (a.out_type == CAT_F32) CAT_LINEAR_LAUNCH(true, CAT_F32);
-        else if (a.out_type == CAT_BF16) CAT_LINEAR_LAUNCH(true, CAT_BF16);
-        else CAT_LINEAR_LAUNCH(true, CAT_F16);
+        if (a.out_type == CAT_F32) CAT_LINEAR_LAUNCH(true, CAT_F32, true);
+        else if (a.out_type == CAT_BF16 && several) CAT_LINEAR_LAUNCH(true, CAT_BF16, true);
+        else if (a.out_type == CAT_BF16) CAT_LINEAR_LAUNCH(true, CAT_BF16, false);
+        else if (several) CAT_LINEAR_LAUNCH(true, CAT_F16, true);
+        else CAT_LINEAR_LAUNCH(true, CAT_F16, false);
     } else {
-        if (a.out_type == CAT_F32) CAT_LINEAR_LAUNCH(false, CAT_F32);
-        else if (a.out_type == CAT_BF16) CAT_LINEAR_LAUNCH(false, CAT_BF16);
-        else CAT_LINEAR_LAUNCH(false, CAT_F16);
+        if (a.out_type == CAT_F32) CAT_LINEAR_LAUNCH(false, CAT_F32, true);
+        else if (a.out_type == CAT_BF16 && several) CAT_LINEAR_LAUNCH(false, CAT_BF16, true);
+        else if (a.out_type == CAT_BF16) CAT_LINEAR_LAUNCH(false, CAT_BF16, false);
+        else if (several) CAT_LINEAR_LAUNCH(false, CAT_F16, true);
+        else CAT_LINEAR_LAUNCH(false, CAT_F16, false);
     }
 #undef CAT_LINEAR_LAUNCH
     count_launch();

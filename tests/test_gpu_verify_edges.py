@@ -1,0 +1,123 @@
+"""cat_verify_drafts at the ends of its ranges: temperatures down to the smallest float, entries at the 2^-1000 where mass ends, rows far from
+nought, calls from several host threads, workspaces as they come."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2509_26277_b200 import binding as B
+from tests.test_gpu_verify import BF, F32, FH, agree, host, problem
+
+pytestmark = pytest.mark.gpu
+
+LN2 = float(np.log(2.0))
+
+
+@pytest.mark.parametrize("T", [1e-37, 4.3e-39, 4.1e-39, 1e-39, 1e-42, 1.4e-45])
+@pytest.mark.parametrize("b,v", [(24, 3000), (3, 50_001)])
+def test_temperatures_down_to_the_smallest_float(T, b, v):
+    """All mass on the largest entry (softmax(logits / T) is defined for every T > 0); and logits as small as T, whose rows are spread as ever."""
+    for target, draft in [(F32, BF), (BF, F32), (F32, None)]:
+        p = problem(b, 2, v, target, draft)
+        p["temperature"][:] = T
+        tokens, _ = agree(p)
+        assert (tokens[:, 0] >= 0).all()
+    p = problem(b, 2, v, F32, F32)
+    p["temperature"][:] = T
+    p["target"], p["draft"] = p["target"] * T, p["draft"] * T
+    agree(p)
+
+
+@pytest.mark.parametrize("T", [1.0, 3e38, float("inf")])
+def test_rows_that_span_all_floats(T):
+    """Entries at both ends of fp32 with temperatures as large: differences of logits pass the largest float, their quotients do not."""
+    p = problem(12, 1, 700, F32, F32, greedy_every=0)
+    p["temperature"][:] = T
+    p["target"][:, :, ::2], p["target"][:, :, 1::2] = 3.4e38, -3.4e38
+    p["draft"][:, :, ::2], p["draft"][:, :, 1::2] = -3.4e38, 3.4e38
+    p["draft_tokens"][::2] = 1
+    agree(p)
+    p["u_sample"][:] = 0
+    p["target"][:, :, :4] = -3.4e38
+    p["draft_lengths"][:] = 0
+    tokens, _ = B.cat_verify_drafts(**p)
+    assert (host(tokens)[:, 0] == (4 if T == 1.0 else 0)).all()
+
+
+@pytest.mark.parametrize("b,v", [(1, 2000), (40, 2000), (200, 2000), (200, 40_000), (3, 40_000)])
+@pytest.mark.parametrize("top", [-420.0, 0.0, 346.0])
+def test_mass_ends_relative_to_the_rows_largest(b, v, top):
+    """u = 0 draws the first entry with mass: one of 2^-900 of its row's largest has some, one of 2^-1100 has none, wherever the largest lies."""
+    g = torch.Generator(device="cuda").manual_seed(v + b)
+    row = top - 4000 - 100 * torch.rand((b, 2, v), generator=g, device="cuda")
+    row[:, :, 3], row[:, :, 5], row[:, :, 9] = top - 1100 * LN2, top - 900 * LN2, top
+    none = torch.full((b, 1, v), -torch.inf, device="cuda")
+    zero, one = torch.zeros((b,), device="cuda"), torch.ones((b, 1), device="cuda")
+    drafts = torch.full((b, 1), 9, dtype=torch.int32, device="cuda")
+    # plain sampling; a refused draft that is the largest entry; one of a draft row without mass, refused since 3 has none itself
+    tokens, kept = B.cat_verify_drafts(row[:, :1], None, drafts[:, :0].contiguous(), one[:, :0].contiguous(), zero)
+    assert (tokens[:, 0] == 5).all()
+    tokens, kept = B.cat_verify_drafts(row, None, torch.full_like(drafts, v), one, zero)
+    assert (tokens[:, 0] == 5).all() and not kept.any()
+    tokens, kept = B.cat_verify_drafts(row, none, torch.full_like(drafts, 3), one, zero)
+    assert (tokens[:, 0] == 5).all() and not kept.any()
+    tokens, kept = B.cat_verify_drafts(row, none, torch.full_like(drafts, 5), one, zero)
+    assert (tokens[:, 0] == 5).all() and (kept == 1).all() and (tokens[:, 1] == 5).all()
+
+
+@pytest.mark.parametrize("b,v", [(1, 500), (40, 2000), (200, 2000), (3, 40_000), (160, 40_000), (60, 90_000)])
+@pytest.mark.parametrize("target", [F32, BF])
+def test_drafts_at_the_end_of_mass_against_rows_without_any(b, v, target):
+    """A draft whose target entry lies next to 2^-1000 of its row's largest, from a draft row that is masked whole: refused just below, accepted just
+    above; the refused one's token is drawn from the target's row."""
+    p = problem(b, 2, v, target, F32, sharp=1.0, greedy_every=0)
+    p["temperature"], p["draft_lengths"] = None, None
+    t = p["target"]
+    t.copy_((t.float() - t.float().amax(-1, keepdim=True)).to(target))
+    p["draft"][:] = -torch.inf
+    p["draft_tokens"][:, 0], p["draft_tokens"][:, 1] = 7, 11
+    for first, second in [(1000.5, 1000.5), (999.5, 1000.5), (1003.0, 999.5), (999.5, 999.5)]:
+        # (one step of bf16 here is 4: the values that it has are 692 = 998.35 ln 2 and 696 = 1004.1 ln 2)
+        t[:, 0, 7], t[:, 1, 11] = -first * LN2, -second * LN2
+        tokens, kept = agree(p)
+        if target == F32:
+            assert (kept == (0 if first > 1000 else 1 if second > 1000 else 2)).all()
+        assert (tokens[np.arange(b), kept] >= 0).all()
+
+
+def test_calls_from_several_host_threads():
+    """Vocabularies whose calls want different amounts of shared memory of the same kernel, from threads at once."""
+    import threading
+
+    work = []
+    for v in (32_000, 50_000, 16_000, 40_000):
+        p = problem(8, 4, v, BF, BF)
+        work.append((p, B.cat_verify_drafts(**p)))
+    agree(work[0][0], got=work[0][1])
+    torch.cuda.synchronize()
+    failures = []
+
+    def loop(p, want):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(400):
+                    got = B.cat_verify_drafts(**p)
+                torch.cuda.current_stream().synchronize()
+                assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        except BaseException as e:      # (an assertion in a thread is lost otherwise)
+            failures.append(e)
+
+    threads = [threading.Thread(target=loop, args=w) for w in work for _ in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failures, failures[0]
+
+
+@pytest.mark.parametrize("b,v", [(4, 1000), (200, 40_000)])
+def test_the_status_of_a_workspace_as_it_comes(b, v):
+    """The status word is this call's, whatever the workspace held."""
+    ws = torch.full((256,), 255, dtype=torch.uint8, device="cuda")
+    p = problem(b, 1, v, BF, BF)
+    agree(p, got=B.cat_verify_drafts(**p, ws=ws))
+    assert B.cat_workspace_report(ws)["device_status"] == 0
