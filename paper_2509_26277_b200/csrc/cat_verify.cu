@@ -606,9 +606,12 @@ __device__ __forceinline__ void weights_f64(const double *table, const float (&x
     int beyond[N];
     const float cf = (float)c;
     const bool ordinary = cf > 1e-15f && cf < 1e15f;
+    // (z - m) c in three steps, none of which overflows before the product would pass 1000 (c from 1e-300 to 2^150, z and m over all of fp32) or gives a
+    // number where z = m but nought; a masked z gives -inf, or NaN
+    const float before = c < 1.0 ? 0.5f : 1.f, between = c > 0x1p100 ? 0x1p40f : 1.f, after = (float)(c / ((double)before * (double)between));
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        const float z = clean(x[k]), at = (z - m) * cf;
+        const float z = clean(x[k]), at = fmaf(z, before, -m * before) * between * after;
         const bool fits = at > -1000.f && at < 1000.f;
         beyond[k] = fits ? 0 : at >= 1000.f ? 2 : 1;      // (a reference that does not suit the row shows in the sum)
         const float y = fits ? z : m;
