@@ -612,7 +612,7 @@ __device__ __forceinline__ void weights_f64(const double *table, const float (&x
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const float z = clean(x[k]), at = fmaf(z, before, -m * before) * between * after;
-        const bool fits = at > -1000.f && at < 1000.f;
+        const bool fits = at > -1001.f && at < 1000.f;
         beyond[k] = fits ? 0 : at >= 1000.f ? 2 : 1;      // (a reference that does not suit the row shows in the sum)
         const float y = fits ? z : m;
         const uint32_t f = __float_as_uint(y);
@@ -625,6 +625,9 @@ __device__ __forceinline__ void weights_f64(const double *table, const float (&x
     for (int k = 0; k < N; ++k) asm volatile("sub.rn.f64 %0, %0, %1;" : "+d"(e[k]) : "d"(md));
 #pragma unroll
     for (int k = 0; k < N; ++k) asm volatile("mul.rn.f64 %0, %0, %1;" : "+d"(e[k]) : "d"(c));
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        if (e[k] < -1000.0) beyond[k] = 1;
 #pragma unroll
     for (int k = 0; k < N; ++k) asm volatile("fma.rn.f64 %0, %1, %2, %3;" : "=d"(t[k]) : "d"(e[k]), "d"(64.0), "d"(6755399441055744.0));   // 1.5 2^52: rounded
 #pragma unroll
@@ -737,10 +740,16 @@ struct Settle {
             wq[k] = q_row ? kept[(4 + k) * room + g - g_cta] : 0.0;
         }
     }
-    // sums of the rows' weights
-    __device__ void normalisers(double &zt, double &zq)
+    // Sums of the rows' weights.  `exact_end`: entries below 2^-1000 of their row's largest, and only those, weigh nothing.
+    __device__ void normalisers(double &zt, double &zq, bool exact_end)
     {
-        for (int attempt = 0;; ++attempt) {
+        for (bool looked_up = false;; looked_up = true) {
+            if (looked_up || exact_end) {
+                m[0] = largest<TT>(t_row, 0);
+                m[1] = q_row ? largest<QT>(q_row, 1) : 0.f;
+                if (m[0] == -CUDART_INF_F) m[0] = 0.f;
+                if (m[1] == -CUDART_INF_F) m[1] = 0.f;
+            }
             zt = zq = 0;
 #pragma unroll 1
             for (int g = g_first + lane; g < g_end; g += 32) {
@@ -757,13 +766,10 @@ struct Settle {
                 }
             }
             sums(zt, zq);
-            // With logits / T within some hundreds of zero, nought is as good a reference as the row's largest.  Else they are looked up.
+            // With logits / T within some hundreds of zero, nought is as good a reference as the row's largest: what either drops is less than any
+            // u times the mass, u = 0 apart.  Else they are looked up.
             const bool suits = zt > 1e-200 && zt < 1e270 && (!q_row || (zq > 1e-200 && zq < 1e270));
-            if (suits || attempt == 1) return;
-            m[0] = largest<TT>(t_row, 0);
-            m[1] = q_row ? largest<QT>(q_row, 1) : 0.f;
-            if (m[0] == -CUDART_INF_F) m[0] = 0.f;
-            if (m[1] == -CUDART_INF_F) m[1] = 0.f;
+            if (suits || looked_up || exact_end) return;
         }
     }
     // whether a logit's weight is less than 2^-1000 of its row's largest, which is between the row's sum and a V-th (2^-22) of it
@@ -805,6 +811,7 @@ __device__ __noinline__ void settle_sequence(const VerifyParams &p, SettleShared
     Settle<TT, QT> c(a, sh, kept, size, a.temperature ? (double)a.temperature[b] : 1.0);
     const int lane = c.lane;
     const bool writer = c.rank == 0 && threadIdx.x == 0;
+    const double u_sample = uniform(a.u_sample[b]);       // (0: the draw is the first entry with any mass)
     if (writer) atomicAdd(reinterpret_cast<unsigned long long *>(&p.ctl->refined_total), 1ull);
     int32_t *out = a.tokens_out + (int64_t)b * (a.S + 1);
     double zt, zq;
@@ -813,7 +820,7 @@ __device__ __noinline__ void settle_sequence(const VerifyParams &p, SettleShared
     for (;; ++j) {
         c.rows(row_of(a.target, TT, b, j, a.target_seq, a.target_row),
                a.draft && j < length ? row_of(a.draft, QT, b, j, a.draft_seq, a.draft_row) : nullptr);
-        c.normalisers(zt, zq);
+        c.normalisers(zt, zq, u_sample == 0.0);
         if (j == length) break;
         x = a.tokens[(int64_t)b * a.S + j];
         const bool inside = x >= 0 && x < a.V;
@@ -866,7 +873,7 @@ __device__ __noinline__ void settle_sequence(const VerifyParams &p, SettleShared
             }
         }
         // the CTA, the warp, the entry at which the sum passes u times the whole; roundings apart: the last with mass
-        const double goal = uniform(a.u_sample[b]) * total;
+        const double goal = u_sample * total;
         auto passes = [&](double v, double &below) {
             const double run = warp_scan(v, lane);
             const unsigned over = __ballot_sync(0xffffffffu, v > 0 && below + run > goal), any = __ballot_sync(0xffffffffu, v > 0);

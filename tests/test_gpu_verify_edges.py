@@ -1,10 +1,14 @@
 """cat_verify_drafts at the ends of its ranges."""
+import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_verify import BF, F32, agree, problem
+from paper_2509_26277_b200 import binding as B
+from tests.test_gpu_verify import BF, F32, agree, host, problem
 
 pytestmark = pytest.mark.gpu
+
+LN2 = float(np.log(2.0))
 
 
 @pytest.mark.parametrize("T", [1e-37, 4.3e-39, 4.1e-39, 1e-39, 1e-42, 1.4e-45])
@@ -31,3 +35,34 @@ def test_rows_that_span_all_floats(T):
     p["draft"][:, :, ::2], p["draft"][:, :, 1::2] = -3.4e38, 3.4e38
     p["draft_tokens"][::2] = 1
     agree(p)
+    p["u_sample"][:] = 0
+    p["target"][:, :, :4] = -3.4e38
+    p["draft_lengths"][:] = 0
+    tokens, _ = B.cat_verify_drafts(**p)
+    assert (host(tokens)[:, 0] == (4 if T == 1.0 else 0)).all()
+
+
+@pytest.mark.parametrize("b,v", [(1, 2000), (40, 2000), (200, 2000), (200, 40_000), (3, 40_000)])
+@pytest.mark.parametrize("top", [-420.0, 0.0, 346.0])
+def test_mass_ends_relative_to_the_rows_largest(b, v, top):
+    """u = 0 draws the first entry with mass: one of 2^-900 of its row's largest has some, one of 2^-1100 has none, wherever the largest lies."""
+    g = torch.Generator(device="cuda").manual_seed(v + b)
+    row = top - 4000 - 100 * torch.rand((b, 2, v), generator=g, device="cuda")
+    row[:, :, 3], row[:, :, 5], row[:, :, 9] = top - 1100 * LN2, top - 900 * LN2, top
+    none = torch.full((b, 1, v), -torch.inf, device="cuda")
+    zero, one = torch.zeros((b,), device="cuda"), torch.ones((b, 1), device="cuda")
+    drafts = torch.full((b, 1), 9, dtype=torch.int32, device="cuda")
+    # plain sampling; a refused draft that is the largest entry; one of a draft row without mass, refused since 3 has none itself
+    tokens, kept = B.cat_verify_drafts(row[:, :1], None, drafts[:, :0].contiguous(), one[:, :0].contiguous(), zero)
+    assert (tokens[:, 0] == 5).all()
+    tokens, kept = B.cat_verify_drafts(row, None, torch.full_like(drafts, v), one, zero)
+    assert (tokens[:, 0] == 5).all() and not kept.any()
+    tokens, kept = B.cat_verify_drafts(row, none, torch.full_like(drafts, 3), one, zero)
+    assert (tokens[:, 0] == 5).all() and not kept.any()
+    tokens, kept = B.cat_verify_drafts(row, none, torch.full_like(drafts, 5), one, zero)
+    assert (tokens[:, 0] == 5).all() and (kept == 1).all() and (tokens[:, 1] == 5).all()
+    # the numbers of fp32 on both sides of 2^-1000
+    if top == 0.0:
+        row[:, :, 3], row[:, :, 5] = -693.14722, -693.14716      # (2^-1000.00006 and 2^-999.99997)
+        tokens, kept = B.cat_verify_drafts(row[:, :1], None, drafts[:, :0].contiguous(), one[:, :0].contiguous(), zero)
+        assert (tokens[:, 0] == 5).all()
