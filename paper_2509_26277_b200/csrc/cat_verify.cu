@@ -315,7 +315,8 @@ struct SettleShared {
     int claim[2];                           // the sequence that the cluster works on, and the row it goes on from
     double part[2][VF_THREADS / 32];        // the warps' parts of two sums over the cluster ...
     double cta[2][2];                       // ... and the CTA's (two sets in turn: an exchange is one barrier)
-    float top[2][2];                        // largest logits of two rows, as far as this CTA has them
+    float top[VF_THREADS / 32];             // the warps' largest logits of a row ...
+    float cta_top[2];                       // ... and the CTA's (two sets in turn; apart from the sums, which a draw goes on from)
 };
 
 struct VerifyShared {
@@ -661,7 +662,7 @@ struct Settle {
     SettleShared &sh;
     double *kept;                    // [row][entry of four][unit]: the weights, where they find room (else null)
     const void *t_row, *q_row;       // q_row: null where there is none
-    int rank, size, warps, warp, lane, turn = 0;
+    int rank, size, warps, warp, lane, turn = 0, top_turn = 0;
     int offset, g_cta, room, g_first, g_end;
     float m[2] = {0.f, 0.f};         // what the weights of the rows are relative to
     double c;
@@ -745,8 +746,8 @@ struct Settle {
     {
         for (bool looked_up = false;; looked_up = true) {
             if (looked_up || exact_end) {
-                m[0] = largest<TT>(t_row, 0);
-                m[1] = q_row ? largest<QT>(q_row, 1) : 0.f;
+                m[0] = largest<TT>(t_row);
+                m[1] = q_row ? largest<QT>(q_row) : 0.f;
                 if (m[0] == -CUDART_INF_F) m[0] = 0.f;
                 if (m[1] == -CUDART_INF_F) m[1] = 0.f;
             }
@@ -774,13 +775,13 @@ struct Settle {
     }
     // whether a logit's weight is less than 2^-1000 of its row's largest, which is between the row's sum and a V-th (2^-22) of it
     template <int TYPE>
-    __device__ bool vanishes(const void *row, int which, float x, double log_mass)
+    __device__ bool vanishes(const void *row, float x, double log_mass)
     {
         if (log_mass > -1000.0 || log_mass < -1023.0) return log_mass < -1000.0;
-        return ((double)x - (double)largest<TYPE>(row, which)) * c < -1000.0;
+        return ((double)x - (double)largest<TYPE>(row)) * c < -1000.0;
     }
     template <int TYPE>
-    __device__ float largest(const void *row, int which)
+    __device__ float largest(const void *row)
     {
         float top = -CUDART_INF_F;
 #pragma unroll 1
@@ -790,15 +791,15 @@ struct Settle {
             top = fmaxf(top, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
         }
         top = clean(warp_max(top));
-        if (lane == 0) sh.part[which][warp] = (double)top;
-        turn ^= 1;
+        if (lane == 0) sh.top[warp] = top;
+        top_turn ^= 1;
         __syncthreads();
         if (warp == 0) {
-            const float t = warp_max(lane < warps ? (float)sh.part[which][lane] : -CUDART_INF_F);
-            if (lane == 0) sh.top[turn][which] = t;
+            const float t = warp_max(lane < warps ? sh.top[lane] : -CUDART_INF_F);
+            if (lane == 0) sh.cta_top[top_turn] = t;
         }
         sync_cluster();
-        return warp_max(lane < size ? peer_f32(&sh.top[turn][which], (uint32_t)lane) : -CUDART_INF_F);
+        return warp_max(lane < size ? peer_f32(&sh.cta_top[top_turn], (uint32_t)lane) : -CUDART_INF_F);
     }
 };
 
@@ -827,8 +828,8 @@ __device__ __noinline__ void settle_sequence(const VerifyParams &p, SettleShared
         // u q < p by logarithms: either may be smaller than any number of fp64
         const float xt = inside && zt > 0 ? logit(c.t_row, x, TT) : -CUDART_INF_F, xq = a.draft && inside && zq > 0 ? logit(c.q_row, x, QT) : -CUDART_INF_F;
         const double log_p = ((double)xt - (double)c.m[0]) * c.c - log2(zt), log_q = a.draft ? ((double)xq - (double)c.m[1]) * c.c - log2(zq) : 0.0;
-        const bool no_p = xt == -CUDART_INF_F || c.template vanishes<TT>(c.t_row, 0, xt, log_p);
-        const bool no_q = a.draft ? xq == -CUDART_INF_F || c.template vanishes<QT>(c.q_row, 1, xq, log_q) : !inside;
+        const bool no_p = xt == -CUDART_INF_F || c.template vanishes<TT>(c.t_row, xt, log_p);
+        const bool no_q = a.draft ? xq == -CUDART_INF_F || c.template vanishes<QT>(c.q_row, xq, log_q) : !inside;
         refused = no_p || !(no_q || log2(uniform(a.u_accept[(int64_t)b * a.S + j])) + log_q < log_p);
         if (refused) break;
         if (writer) out[j] = x;

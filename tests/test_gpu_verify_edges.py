@@ -66,3 +66,23 @@ def test_mass_ends_relative_to_the_rows_largest(b, v, top):
         row[:, :, 3], row[:, :, 5] = -693.14722, -693.14716      # (2^-1000.00006 and 2^-999.99997)
         tokens, kept = B.cat_verify_drafts(row[:, :1], None, drafts[:, :0].contiguous(), one[:, :0].contiguous(), zero)
         assert (tokens[:, 0] == 5).all()
+
+
+@pytest.mark.parametrize("b,v", [(1, 500), (40, 2000), (200, 2000), (3, 40_000), (160, 40_000), (60, 90_000)])
+@pytest.mark.parametrize("target", [F32, BF])
+def test_drafts_at_the_end_of_mass_against_rows_without_any(b, v, target):
+    """A draft whose target entry lies next to 2^-1000 of its row's largest, from a draft row that is masked whole: refused just below, accepted just
+    above; the refused one's token is drawn from the target's row."""
+    p = problem(b, 2, v, target, F32, sharp=1.0, greedy_every=0)
+    p["temperature"], p["draft_lengths"] = None, None
+    t = p["target"]
+    t.copy_((t.float() - t.float().amax(-1, keepdim=True)).to(target))
+    p["draft"][:] = -torch.inf
+    p["draft_tokens"][:, 0], p["draft_tokens"][:, 1] = 7, 11
+    for first, second in [(1000.5, 1000.5), (999.5, 1000.5), (1003.0, 999.5), (999.5, 999.5)]:
+        # (one step of bf16 here is 4: the values that it has are 692 = 998.35 ln 2 and 696 = 1004.1 ln 2)
+        t[:, 0, 7], t[:, 1, 11] = -first * LN2, -second * LN2
+        tokens, kept = agree(p)
+        if target == F32:
+            assert (kept == (0 if first > 1000 else 1 if second > 1000 else 2)).all()
+        assert (tokens[np.arange(b), kept] >= 0).all()
