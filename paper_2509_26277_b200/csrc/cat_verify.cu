@@ -1269,13 +1269,16 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
     }
 }
 
+// The limit of a kernel's dynamic shared memory is the kernel's, not the call's: every call sets the same, or one from another thread could find a
+// smaller one than it needs.
+constexpr int VF_MAX_SMEM = 200 * 1024;
+
 template <int TT, int QT>
 cudaError_t launch_fast(const VerifyParams &p, cudaLaunchConfig_t &cfg)
 {
     auto kern = p.vecs == 4 ? verify_kernel<TT, QT, 4> : verify_kernel<TT, QT, 1>;
     cudaError_t e;
-    if (cfg.dynamicSmemBytes > 40 * 1024 &&
-        (e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)) != cudaSuccess)
+    if (cfg.dynamicSmemBytes > 40 * 1024 && (e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, VF_MAX_SMEM)) != cudaSuccess)
         return e;
     return cudaLaunchKernelEx(&cfg, kern, p);
 }
@@ -1285,7 +1288,7 @@ cudaError_t launch_settle(const VerifyParams &p, cudaLaunchConfig_t &cfg)
 {
     cudaError_t e;
     if ((e = cudaFuncSetAttribute(verify_settle_kernel<TT, QT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
-    if ((e = cudaFuncSetAttribute(verify_settle_kernel<TT, QT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024)) != cudaSuccess) return e;
+    if ((e = cudaFuncSetAttribute(verify_settle_kernel<TT, QT>, cudaFuncAttributeMaxDynamicSharedMemorySize, VF_MAX_SMEM)) != cudaSuccess) return e;
     return cudaLaunchKernelEx(&cfg, verify_settle_kernel<TT, QT>, p);
 }
 
@@ -1327,7 +1330,7 @@ cudaError_t launch_verify(const VerifyArgs &a, void *workspace, cudaStream_t s)
     // (the weights of two rows in fp64: where a CTA has an SM to itself, or they are small)
     auto kept_bytes = [&](int size) { return ((entries + 6) / 4 / size + 1) * 64; };
     size_t smem = (size_t)p.slots * 12;
-    p.keep = p.settle && (kept_bytes(p.size) <= 16 * 1024 || ((int64_t)a.B * p.size <= sms && kept_bytes(p.size) <= 200 * 1024));
+    p.keep = p.settle && (kept_bytes(p.size) <= 16 * 1024 || ((int64_t)a.B * p.size <= sms && kept_bytes(p.size) <= VF_MAX_SMEM));
     if (p.keep && smem < (size_t)kept_bytes(p.size)) smem = (size_t)kept_bytes(p.size);
 
     cudaLaunchConfig_t cfg{};
@@ -1355,7 +1358,7 @@ cudaError_t launch_verify(const VerifyArgs &a, void *workspace, cudaStream_t s)
     if (e != cudaSuccess || p.settle) return e;
 
     p.size = VF_SETTLE_CLUSTER;
-    p.keep = kept_bytes(p.size) <= 200 * 1024;
+    p.keep = kept_bytes(p.size) <= VF_MAX_SMEM;
     const int clusters = a.B < sms / p.size ? a.B : sms / p.size;
     cfg.gridDim = dim3((unsigned)(clusters * p.size), 1, 1);
     cfg.blockDim = dim3(VF_THREADS, 1, 1);

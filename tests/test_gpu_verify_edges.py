@@ -86,3 +86,35 @@ def test_drafts_at_the_end_of_mass_against_rows_without_any(b, v, target):
         if target == F32:
             assert (kept == (0 if first > 1000 else 1 if second > 1000 else 2)).all()
         assert (tokens[np.arange(b), kept] >= 0).all()
+
+
+def test_calls_from_several_host_threads():
+    """Vocabularies whose calls want different amounts of shared memory of the same kernel (64 to 127 KB), from threads that do nothing but call."""
+    import threading
+
+    failures = []
+
+    def loop(v):
+        try:
+            p = problem(8, 4, v, BF, BF)
+            want = B.cat_verify_drafts(**p)
+            tokens, kept = torch.empty_like(want[0]), torch.empty_like(want[1])
+            ws = torch.zeros(256, dtype=torch.uint8, device="cuda")
+            stream = torch.cuda.Stream()
+            torch.cuda.synchronize()
+            at = lambda t: t.data_ptr()
+            args = (at(p["target"]), 1, 5 * v, v, at(p["draft"]), 1, 4 * v, v, at(p["draft_tokens"]), at(p["draft_lengths"]), at(p["temperature"]),
+                    at(p["u_accept"]), at(p["u_sample"]), 8, 4, v, at(tokens), at(kept), at(ws), 256, stream.cuda_stream)
+            call = B.lib().cat_verify_drafts
+            assert [s for s in (call(*args) for _ in range(3000)) if s] == []
+            stream.synchronize()
+            assert torch.equal(tokens, want[0]) and torch.equal(kept, want[1])
+        except BaseException as e:      # (an assertion in a thread is lost otherwise)
+            failures.append(e)
+
+    threads = [threading.Thread(target=loop, args=(v,)) for v in (32_000, 48_000, 40_000, 63_000)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failures, str(failures[0])[:300]
