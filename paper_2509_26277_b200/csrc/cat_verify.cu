@@ -310,9 +310,44 @@ __device__ __forceinline__ float sum_of(const float (&w)[N])
     return a + b;
 }
 
+// What a sequence's control flow hangs on is read once, by its cluster's first CTA, and reaches the others through shared memory: whatever a
+// caller does to its inputs meanwhile, all take the same way and meet at the same barriers.
+struct Head {
+    float T, u_sample;
+    int length;
+};
+__device__ __forceinline__ Head read_head(const VerifyArgs &a, int b)
+{
+    return Head{a.temperature ? a.temperature[b] : 1.f, a.u_sample[b], a.lengths ? min(a.lengths[b], a.S) : a.S};
+}
+__device__ __forceinline__ Head peer_head(const Head *h, uint32_t rank)
+{
+    return Head{peer_f32(&h->T, rank), peer_f32(&h->u_sample, rank), peer_s32(&h->length, rank)};
+}
+// A draft, its uniform number, and its logits in the target's and in the draft's row (-inf for a token outside the vocabulary).
+struct Draft {
+    int x;
+    float u, xt, xq;
+};
+__device__ __forceinline__ Draft read_draft(const VerifyArgs &a, int64_t b, int j, int target_type, int draft_type)
+{
+    Draft d{*(const volatile int32_t *)&a.tokens[b * a.S + j], a.u_accept[b * a.S + j], -CUDART_INF_F, -CUDART_INF_F};      // (x: read once, checked, used)
+    if (d.x >= 0 && d.x < a.V) {
+        d.xt = logit(row_of(a.target, target_type, b, j, a.target_seq, a.target_row), d.x, target_type);
+        if (a.draft) d.xq = logit(row_of(a.draft, draft_type, b, j, a.draft_seq, a.draft_row), d.x, draft_type);
+    }
+    return d;
+}
+__device__ __forceinline__ Draft peer_draft(const Draft *d, uint32_t rank)
+{
+    return Draft{peer_s32(&d->x, rank), peer_f32(&d->u, rank), peer_f32(&d->xt, rank), peer_f32(&d->xq, rank)};
+}
+
 struct SettleShared {
     double table[64];                       // 2^(i / 64)
-    int claim[2];                           // the sequence that the cluster works on, and the row it goes on from
+    int claim[2];                           // the sequence that the cluster works on, and the row it goes on from ...
+    Head head;                              // ... and what it hangs on (the first CTA's)
+    Draft draft[2];                         // the draft of the row at work (likewise; two sets in turn)
     double part[2][VF_THREADS / 32];        // the warps' parts of two sums over the cluster ...
     double cta[2][2];                       // ... and the CTA's (two sets in turn: an exchange is one barrier)
     float top[VF_THREADS / 32];             // the warps' largest logits of a row ...
@@ -321,6 +356,8 @@ struct SettleShared {
 
 struct VerifyShared {
     SettleShared settle;
+    Head head;                        // (the first CTA's, as are the drafts of a round: two sets in turn)
+    Draft draft[2][VF_MAX_GROUP];
     double row_z[2][VF_MAX_ROWS];     // this CTA's part of the rows between two exchanges (two sets in turn) ...
     int row_m[2][VF_MAX_ROWS];        // ... and their exponents; greedy: value and place of the largest entry
     double total_z[VF_MAX_ROWS];      // over the cluster
@@ -805,14 +842,14 @@ struct Settle {
 
 // Sequence b from its row j on (the drafts before stand), by the whole cluster.  Greedy sequences never come here.
 template <int TT, int QT>
-__device__ __noinline__ void settle_sequence(const VerifyParams &p, SettleShared &sh, double *kept, int size, int b, int j)
+__device__ __noinline__ void settle_sequence(const VerifyParams &p, SettleShared &sh, double *kept, int size, int b, int j, Head head)
 {
     const VerifyArgs &a = p.a;
-    const int length = a.lengths ? min(a.lengths[b], a.S) : a.S;
-    Settle<TT, QT> c(a, sh, kept, size, a.temperature ? (double)a.temperature[b] : 1.0);
+    const int length = head.length;
+    Settle<TT, QT> c(a, sh, kept, size, (double)head.T);
     const int lane = c.lane;
     const bool writer = c.rank == 0 && threadIdx.x == 0;
-    const double u_sample = uniform(a.u_sample[b]);       // (0: the draw is the first entry with any mass)
+    const double u_sample = uniform(head.u_sample);       // (0: the draw is the first entry with any mass)
     if (writer) atomicAdd(reinterpret_cast<unsigned long long *>(&p.ctl->refined_total), 1ull);
     int32_t *out = a.tokens_out + (int64_t)b * (a.S + 1);
     double zt, zq;
@@ -821,16 +858,18 @@ __device__ __noinline__ void settle_sequence(const VerifyParams &p, SettleShared
     for (;; ++j) {
         c.rows(row_of(a.target, TT, b, j, a.target_seq, a.target_row),
                a.draft && j < length ? row_of(a.draft, QT, b, j, a.draft_seq, a.draft_row) : nullptr);
+        if (writer && j < length) sh.draft[j & 1] = read_draft(a, b, j, TT, QT);
         c.normalisers(zt, zq, u_sample == 0.0);
-        if (j == length) break;
-        x = a.tokens[(int64_t)b * a.S + j];
+        if (j >= length) break;
+        const Draft d = peer_draft(&sh.draft[j & 1], 0);
+        x = d.x;
         const bool inside = x >= 0 && x < a.V;
         // u q < p by logarithms: either may be smaller than any number of fp64
-        const float xt = inside && zt > 0 ? logit(c.t_row, x, TT) : -CUDART_INF_F, xq = a.draft && inside && zq > 0 ? logit(c.q_row, x, QT) : -CUDART_INF_F;
+        const float xt = zt > 0 ? d.xt : -CUDART_INF_F, xq = zq > 0 ? d.xq : -CUDART_INF_F;
         const double log_p = ((double)xt - (double)c.m[0]) * c.c - log2(zt), log_q = a.draft ? ((double)xq - (double)c.m[1]) * c.c - log2(zq) : 0.0;
         const bool no_p = xt == -CUDART_INF_F || c.template vanishes<TT>(c.t_row, xt, log_p);
         const bool no_q = a.draft ? xq == -CUDART_INF_F || c.template vanishes<QT>(c.q_row, xq, log_q) : !inside;
-        refused = no_p || !(no_q || log2(uniform(a.u_accept[(int64_t)b * a.S + j])) + log_q < log_p);
+        refused = no_p || !(no_q || log2(uniform(d.u)) + log_q < log_p);
         if (refused) break;
         if (writer) out[j] = x;
     }
@@ -960,13 +999,14 @@ __global__ void __launch_bounds__(VF_THREADS, 1) verify_settle_kernel(const __gr
             }
             if (lane == 0) {
                 sh.claim[0] = claim;
-                sh.claim[1] = row;
+                sh.claim[1] = min(row, a.S);
+                if (claim >= 0) sh.head = read_head(a, claim);
             }
         }
         sync_cluster();
         const int b = peer_s32(&sh.claim[0], 0), row = peer_s32(&sh.claim[1], 0);
         if (b < 0) break;
-        settle_sequence<TT, QT>(p, sh, p.keep ? kept : nullptr, p.size, b, row);      // (its barriers lie between this claim's reading and the next one's writing)
+        settle_sequence<TT, QT>(p, sh, p.keep ? kept : nullptr, p.size, b, row, peer_head(&sh.head, 0));      // (its barriers lie between this claim's reading and the next one's writing)
     }
     sync_cluster();
 }
@@ -982,12 +1022,18 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
     const int size = p.size;
     const uint32_t rank = size > 1 ? cta_rank() : 0u;
     const int b = (int)blockIdx.x / size;
-    const float Tf = a.temperature ? a.temperature[b] : 1.f;
-    const int length = a.lengths ? min(a.lengths[b], a.S) : a.S;
-    if (length < 0) return;                 // (all CTAs of the cluster)
+    if (rank == 0 && tid == 0) sh.head = read_head(a, b);
+    if (size > 1) sync_cluster();
+    else __syncthreads();
+    const Head head = peer_head(&sh.head, 0);
+    const int length = head.length;
+    if (length < 0) {                       // (all CTAs of the cluster)
+        if (size > 1) sync_cluster();       // (all have read the first one's shared memory)
+        return;
+    }
     // (These conditions live through the whole kernel.  They are kept in registers on purpose: as conditions, `drafts` was seen lost on the way to
     // its last uses -- CUDA 12.9, sm_100a; test_types fails then.)
-    int greedy = !(Tf > 0.f), decides = warp == warps - 1, drafts = a.draft != nullptr && !greedy;
+    int greedy = !(head.T > 0.f), decides = warp == warps - 1, drafts = a.draft != nullptr && !greedy;
     asm volatile("" : "+r"(greedy), "+r"(decides), "+r"(drafts));
     // chunks of this CTA: of target rows, of draft rows
     const int c0 = (int)((int64_t)p.chunks_t * rank / size), mine = (int)((int64_t)p.chunks_t * (rank + 1) / size) - c0;
@@ -995,7 +1041,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
     int *chunk_m = reinterpret_cast<int *>(chunk_z + p.slots);
     auto target_row = [&](int j) { return row_of(a.target, TT, b, j, a.target_seq, a.target_row); };
     auto draft_row = [&](int j) { return row_of(a.draft, QT, b, j, a.draft_seq, a.draft_row); };
-    const Scale sc(greedy ? 1.0 : (double)Tf);
+    const Scale sc(greedy ? 1.0 : (double)head.T);
 
     int verdict = sc.fits ? VF_GO_ON : VF_UNDECIDED, j = 0, turn = 0, rows_t = 0, j0 = 0, group = p.group;
     if (tid == 0) sh.owner = sh.open = 0;
@@ -1008,16 +1054,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
         const int pairs = min(rows_t, length - j0), rows = rows_t + (drafts ? pairs : 0);
         const int tasks_t = rows_t * mine, tasks = tasks_t + (rows - rows_t) * mine_q;
         // What the decisions take besides the sums is read by the warp that decides, the last one: it has the fewest chunks.
-        int x = -1;
-        float ua = 0.f, xt = -CUDART_INF_F, xq = -CUDART_INF_F;
-        if (decides && lane < pairs) {
-            x = a.tokens[(int64_t)b * a.S + j0 + lane];
-            ua = a.u_accept[(int64_t)b * a.S + j0 + lane];
-            if (x >= 0 && x < a.V) {
-                xt = logit(target_row(j0 + lane), x, TT);
-                if (a.draft) xq = logit(draft_row(j0 + lane), x, QT);
-            }
-        }
+        if (rank == 0 && decides && lane < pairs) sh.draft[turn][lane] = read_draft(a, b, j0 + lane, TT, QT);
         // a warp's tasks are every warps-th chunk of the rows, one after the other
         int row_at = 0, per = mine, c = warp;
         const void *row = target_row(j0);
@@ -1101,8 +1138,11 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
         __syncthreads();
         if (decides) {
             // lane i: draft j0 + i; every CTA of the cluster decides the same from the same numbers
-            int how = VF_ALL_STAND;      // (nothing left to decide)
+            int how = VF_ALL_STAND, x = -1;      // (nothing left to decide)
             if (lane < pairs) {
+                const Draft d = peer_draft(&sh.draft[turn][lane], 0);
+                const float ua = d.u, xt = d.xt, xq = d.xq;
+                x = d.x;
                 const double zt = sh.total_z[lane];
                 const int mt = sh.total_m[lane];
                 if (greedy) {
@@ -1223,7 +1263,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
                 if (size > 1) v = lane < size ? scaled(peer_f64(&sh.row_z[turn][slot], (uint32_t)lane), peer_s32(&sh.row_m[turn][slot], (uint32_t)lane), mt) : 0.0;
                 else v = lane == 0 ? (residual ? sh.row_z[turn][0] : zt) : 0.0;
                 double run = warp_scan(v, lane);
-                const double total = __shfl_sync(0xffffffffu, run, 31), goal = uniform(a.u_sample[b]) * total;
+                const double total = __shfl_sync(0xffffffffu, run, 31), goal = uniform(head.u_sample) * total;
                 // sums of p - q: p and q are off by VF_EPS_P of themselves, and the sums round
                 if (residual) err = 1.01 * 2.0 * (2.0 * VF_EPS_P + 5.0 * VF_U * total);
                 unsigned over = __ballot_sync(0xffffffffu, run > goal);
@@ -1264,7 +1304,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
         if (open) {
             fill_table(sh.settle.table);
             __syncthreads();
-            settle_sequence<TT, QT>(p, sh.settle, p.keep ? chunk_z : nullptr, size, b, j);
+            settle_sequence<TT, QT>(p, sh.settle, p.keep ? chunk_z : nullptr, size, b, j, head);
         }
     }
 }

@@ -118,3 +118,36 @@ def test_calls_from_several_host_threads():
     for t in threads:
         t.join()
     assert not failures, str(failures[0])[:300]
+
+
+@pytest.mark.parametrize("b,s,v", [(1, 3, 1000), (8, 4, 32_000), (30, 6, 20_000), (200, 3, 2000), (64, 5, 100_000), (300, 0, 5000)])
+def test_inputs_that_change_during_calls(b, s, v):
+    """What a call reads then is either value; it ends all the same, and its tokens are tokens."""
+    p = problem(b, s, v, BF, BF)
+    g = torch.Generator(device="cuda").manual_seed(v)
+    rand = lambda *shape: torch.rand(shape, generator=g, device="cuda")
+    sets = []
+    for i in range(8):
+        T = 2 * rand(b)
+        T[rand(b) < 0.2], T[rand(b) < 0.1], T[rand(b) < 0.1] = 0.0, 1e-40, 1e30
+        u, a = rand(b), rand(b, s)
+        u[rand(b) < 0.2], a[rand(b, s) < 0.2] = 0.0, float("nan")
+        x = (rand(b, s) * v).int()
+        x[rand(b, s) < 0.1] = -5
+        keep = rand(b, s) < 0.7
+        x[keep] = p["draft_tokens"][keep]
+        n = torch.randint(-1, s + 2, (b,), generator=g, device="cuda", dtype=torch.int32)
+        sets.append(dict(temperature=T, u_sample=u, u_accept=a, draft_tokens=x, draft_lengths=n))
+    here, side = torch.cuda.Stream(), torch.cuda.Stream()
+    tokens, kept = torch.full((b, s + 1), -1, dtype=torch.int32, device="cuda"), torch.zeros((b,), dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    for i in range(150):
+        with torch.cuda.stream(here):
+            B.cat_verify_drafts(**p, tokens_out=tokens, accepted_out=kept)
+        with torch.cuda.stream(side):
+            for k, x in sets[i % 8].items():
+                p[k].copy_(x)
+    torch.cuda.synchronize()
+    assert int(tokens.min()) >= -1 and int(tokens.max()) < v
+    p["draft_lengths"][:] = s
+    agree(p, allow=b)
