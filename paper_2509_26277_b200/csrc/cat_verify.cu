@@ -362,10 +362,12 @@ struct VerifyShared {
     int row_m[2][VF_MAX_ROWS];        // ... and their exponents; greedy: value and place of the largest entry
     double total_z[VF_MAX_ROWS];      // over the cluster
     int total_m[VF_MAX_ROWS];
-    int verdict, at, x;               // what the round decided, for which row, and the draft there
+    int verdict, at, x;               // what the round decided, for which row, and the draft there;
+    int source, token;                // what the token behind the accepted drafts is drawn from, or (VF_FROM_NOTHING) the token
     int owner, open;                  // the CTA that draws; there: the draw came too close to a border
 };
 enum { VF_GO_ON = 0, VF_REFUSED = 1, VF_ALL_STAND = 2, VF_UNDECIDED = 3 };
+enum { VF_FROM_NOTHING = 0, VF_FROM_ROW = 1, VF_FROM_DIFFERENCE = 2 /* p - q */, VF_FROM_OTHERS = 3 /* p without a refused draft from a lookup */ };
 
 // z 2^(m - M), m <= M
 __device__ __forceinline__ double scaled(double z, int m, int M)
@@ -572,14 +574,14 @@ __device__ __forceinline__ void chunk_masses(const Source &src, const Scale &sc,
     load_chunk<TT, VECS>(src.t_row, chunk, V, lane, tv);
     const int first = (chunk * (32 * VECS) + lane) * L::PER - row_offset<TT>(src.t_row);
     Words<L::PER * Logits<QT>::SIZE / 4> qv[VECS];
-    float x[L::PER], w[L::PER];
+    float x[L::PER], w[L::PER];     // (qv and x are looked at where there is a draft's row only)
     if (src.q_row) {
 #pragma unroll
         for (int q = 0; q < VECS; ++q) qv[q] = words_of<QT, L::PER>(src.q_row, first + q * 32 * L::PER, V);
     }
 #pragma unroll
     for (int q = 0; q < VECS; ++q) {
-        entries<QT, L::PER>(qv[q], x);
+        if (src.q_row) entries<QT, L::PER>(qv[q], x);
         masses_of<TT>(src, sc, wt, wq, first + q * 32 * L::PER, V, tv[q], x, w);
         sum[q] = sum_of<L::PER>(w);
     }
@@ -1031,10 +1033,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
         if (size > 1) sync_cluster();       // (all have read the first one's shared memory)
         return;
     }
-    // (These conditions live through the whole kernel.  They are kept in registers on purpose: as conditions, `drafts` was seen lost on the way to
-    // its last uses -- CUDA 12.9, sm_100a; test_types fails then.)
-    int greedy = !(head.T > 0.f), decides = warp == warps - 1, drafts = a.draft != nullptr && !greedy;
-    asm volatile("" : "+r"(greedy), "+r"(decides), "+r"(drafts));
+    const bool greedy = !(head.T > 0.f), decides = warp == warps - 1, drafts = a.draft != nullptr && !greedy;
     // chunks of this CTA: of target rows, of draft rows
     const int c0 = (int)((int64_t)p.chunks_t * rank / size), mine = (int)((int64_t)p.chunks_t * (rank + 1) / size) - c0;
     const int d0 = (int)((int64_t)p.chunks_q * rank / size), mine_q = (int)((int64_t)p.chunks_q * (rank + 1) / size) - d0;
@@ -1194,6 +1193,19 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
                 sh.verdict = how;
                 sh.at = j0 + first;
                 sh.x = x;
+                if (how == VF_REFUSED || how == VF_ALL_STAND) {
+                    const int mt = sh.total_m[first];
+                    if (greedy || mt <= VF_EMPTY) {
+                        sh.source = VF_FROM_NOTHING;
+                        sh.token = greedy && sh.total_z[first] > -CUDART_INF ? mt : -1;      // (no mass: no token)
+                    } else if (mt >= VF_WILD) {
+                        sh.verdict = VF_UNDECIDED;
+                    } else if (how == VF_REFUSED && !drafts) {
+                        sh.source = VF_FROM_OTHERS;
+                    } else {
+                        sh.source = how == VF_REFUSED && sh.total_m[rows_t + first] > VF_EMPTY ? VF_FROM_DIFFERENCE : VF_FROM_ROW;
+                    }
+                }
             }
         }
         __syncthreads();
@@ -1204,25 +1216,23 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
     // the token behind the accepted drafts
     int32_t *out = a.tokens_out + (int64_t)b * (a.S + 1);
     if (verdict != VF_UNDECIDED) {
-        const int r = j - j0;
-        const int mt = sh.total_m[r];
-        const double zt = sh.total_z[r];
-        if (!greedy && mt >= VF_WILD) {
-            verdict = VF_UNDECIDED;
-        } else if (greedy || mt <= VF_EMPTY) {
+        const int source = sh.source;
+        if (source == VF_FROM_NOTHING) {
             if (rank == 0 && tid == 0) {
-                out[j] = greedy && zt > -CUDART_INF ? mt : -1;      // (no mass: no token)
+                out[j] = sh.token;
                 a.accepted_out[b] = j;
             }
         } else {
+            const int r = j - j0, mt = sh.total_m[r];
+            const double zt = sh.total_z[r];
             Source src{target_row(j), nullptr, 1.f, 1.f, mt, 0, -1};
             int slot = r;                                   // where the masses of the CTAs and of the chunks are
             double err = 1.01 * 2.0 * VF_EPS_SUM * zt;
-            const bool residual = verdict == VF_REFUSED && !(drafts && sh.total_m[rows_t + r] <= VF_EMPTY);
+            const bool residual = source != VF_FROM_ROW;
             if (residual) {
                 // from what the refused draft's row leaves of it: both rows once more.  (Of the row itself the chunks' sums are known.)
                 src.t_scale = 1.f / (float)zt;
-                if (drafts) {
+                if (source == VF_FROM_DIFFERENCE) {
                     src.q_row = draft_row(j);
                     src.q_m = sh.total_m[rows_t + r];
                     src.q_scale = 1.f / (float)sh.total_z[rows_t + r];
