@@ -404,10 +404,11 @@ cat_status_t cat_linear(const void *X, int64_t ldx, const void *W, int64_t ldw, 
  * tokens_out [B, S+1]: the accepted drafts, the drawn token, -1 behind it.  accepted_out [B]: how many were accepted.
  * Logits: -inf (a mask) and NaN have no mass, nor has what is below 2^-1000 of its row's largest; +inf counts as the largest finite number.  A row without any mass accepts
  * nothing and gives token -1.  A residual of less mass than 2^-40 is what rounding left of none: the draw is from p_j then.
- * The outputs are those of fp64 arithmetic: what fast fp32 sums cannot decide within their error bound goes to an fp64 pass
- * (cat_workspace_report counts those sequences).  S = 0 is allowed (draft, draft_tokens and u_accept may be NULL then), B = 0 does nothing.
+ * The outputs are those of fp64 arithmetic: what fast fp32 sums cannot decide within their error bound goes to an fp64 pass.  S = 0 is allowed (draft, draft_tokens and u_accept may be NULL then), B = 0 does nothing.
  * The outputs overlap neither each other nor an input, and lie nowhere between the first and the last of the target's, or the draft's, logits.
- * Limits: B <= CAT_VERIFY_MAX_B, S <= CAT_VERIFY_MAX_S, V <= CAT_VERIFY_MAX_V.  Workspace: CAT_VERIFY_WORKSPACE_BYTES.
+ * Limits: B <= CAT_VERIFY_MAX_B, S <= CAT_VERIFY_MAX_S, V <= CAT_VERIFY_MAX_V.  Workspace: CAT_VERIFY_WORKSPACE_BYTES, a control block.  For
+ * cat_workspace_report each call writes its status and adds the number of sequences that took the fp64 pass to the running total; nothing resets the
+ * total, so a caller who reads it sets the block to zero once before the first call.
  */
 #define CAT_VERIFY_MAX_B (1 << 20)
 #define CAT_VERIFY_MAX_S 256
@@ -458,7 +459,8 @@ cat_status_t cat_fit_host(const float *Yq_host, const float *Yfp_host, int64_t N
  * total since the last cat_fit started on that workspace, and the device status
  * word (CAT_OK or CAT_ERR_DEVICE_TIMEOUT: outputs of that call are undefined).  For the calls that
  * compose several steps -- cat_pca_fit, cat_fit_pca, cat_apply_pca -- the block speaks for all of them.  (The
- * host-buffer calls keep theirs behind their staging buffers, out of this call's reach.) */
+ * host-buffer calls keep theirs behind their staging buffers, out of this call's reach.)  cat_linear writes the status only, cat_verify_drafts the
+ * status and the running total, of sequences, in a block that its caller has zeroed. */
 cat_status_t cat_workspace_report(const void *workspace, void *stream, int64_t *refined_last_host,
                                   int64_t *refined_total_host, int32_t *device_status_host);
 

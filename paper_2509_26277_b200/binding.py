@@ -640,7 +640,8 @@ def cat_verify_drafts(target, draft, draft_tokens, u_accept, u_sample, draft_len
                       accepted_out=None, ws=None):
     """cat_verify_drafts: (tokens [B, S + 1] int32, accepted [B] int32) for target [B, S + 1, V] and draft [B, S, V] logits (None:
     drafts without probabilities), draft_tokens [B, S] int32, uniform numbers u_accept [B, S] and u_sample [B] fp32, lengths [B]
-    int32 and temperatures [B] fp32 (see cat.h)."""
+    int32 and temperatures [B] fp32 (see cat.h).  A `ws` of one's own is 256 bytes; zero it first to read the sequences that took the fp64
+    pass from cat_workspace_report."""
     device = target.device
     if not target.is_cuda:
         raise TypeError("target must be a CUDA tensor")

@@ -1024,6 +1024,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
     const int size = p.size;
     const uint32_t rank = size > 1 ? cta_rank() : 0u;
     const int b = (int)blockIdx.x / size;
+    if (blockIdx.x == 0 && tid == 0) p.ctl->device_status = CAT_OK;      // (nothing here waits for long)
     if (rank == 0 && tid == 0) sh.head = read_head(a, b);
     if (size > 1) sync_cluster();
     else __syncthreads();

@@ -151,3 +151,20 @@ def test_inputs_that_change_during_calls(b, s, v):
     assert int(tokens.min()) >= -1 and int(tokens.max()) < v
     p["draft_lengths"][:] = s
     agree(p, allow=b)
+
+
+@pytest.mark.parametrize("b,v", [(4, 1000), (200, 40_000)])
+def test_the_status_of_a_workspace_as_it_comes(b, v):
+    """The status word is this call's, whatever the workspace held; the count is the running total over a block that was zeroed."""
+    ws = torch.full((256,), 255, dtype=torch.uint8, device="cuda")
+    p = problem(b, 1, v, F32, F32, sharp=0.1, noise=0.05, greedy_every=0)
+    p["draft_lengths"][0] = -1
+    agree(p, got=B.cat_verify_drafts(**p, ws=ws, tokens_out=torch.full((b, 2), -9, dtype=torch.int32, device="cuda"),
+                                     accepted_out=torch.full((b,), -9, dtype=torch.int32, device="cuda")))
+    assert B.cat_workspace_report(ws)["device_status"] == 0
+    ws.zero_()
+    for i in range(3):
+        B.cat_verify_drafts(**p, ws=ws)
+        if i == 0:
+            once = B.cat_workspace_report(ws)["refined_rows_total"]
+    assert B.cat_workspace_report(ws) == dict(B.cat_workspace_report(ws), device_status=0, refined_rows_total=3 * once)
