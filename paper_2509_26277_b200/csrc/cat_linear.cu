@@ -26,6 +26,7 @@ constexpr int LN_EPI_WARPS = 16;                // warps of the epilogue at most
 constexpr int LN_MAX_THREADS = 32 * (2 + LN_EPI_WARPS);
 constexpr int LN_RUN = 12;                      // slabs per run of an accumulator at most, where the result is fp32 (see linear_kernel) ...
 constexpr int LN_RUN_16 = 24;                   // ... and where it is rounded to 16 bits
+constexpr int LN_TWO = 32;                      // single CTAs of up to that many tokens fit two to an SM: 320 threads of 96 registers, half the shared memory
 constexpr int LN_GROUP = 8;                     // token tiles that share a sweep over the weights
 
 struct LinearParams {
@@ -631,8 +632,8 @@ LinearPlan plan(int64_t M, int N, int K, int sms)
             const float slab = pair ? row.pair : row.single;
             if (slab == 0.f) continue;
             const int64_t tiles = (int64_t)((N + (pair ? 255 : 127)) / (pair ? 256 : 128)) * ((M + row.nt - 1) / row.nt);
-            // (CTAs of up to 64 tokens fit two to an SM, which they then share)
-            const int64_t slots = sms / (pair ? 2 : 1), most = row.nt <= 64 && !pair ? 2 * slots : slots;
+            // (two CTAs share an SM where they fit)
+            const int64_t slots = sms / (pair ? 2 : 1), most = row.nt <= LN_TWO && !pair ? 2 * slots : slots;
             for (int splits = 1; splits <= (pair ? 2 : row.nt <= 64 ? 8 : 4) && splits * 2 <= (slabs > 1 ? slabs : 2); splits *= 2) {
                 if (splits > 1 && tiles * splits > most) break;
                 const float waves = (float)((tiles * splits + slots - 1) / slots);
@@ -719,14 +720,15 @@ cudaError_t launch_linear(const LinearArgs &a, void *workspace, cudaStream_t s)
     const int stage_bytes = TC_A_BYTES + p.nt_cta * TC_SLAB_BYTES;
     const int64_t units = (int64_t)p.tiles_w * p.tiles_t;
     // With few tokens half an SM's shared memory holds more than enough slabs in flight (100 KB; the memory wants about 45), and the next call's
-    // CTAs can settle in beside these.
-    const int room_smem = (pl.nt <= 64 && !pl.pair ? 113 : 227) * 1024 - 2048 - (int)sizeof(LinearShared);
+    // CTAs can settle in beside these.  From 33 tokens on (576 threads) they cannot, and the whole of it is taken: 64 x 28672 x 4096 48.5 us, 54.9 with half
+    // of it.
+    const int room_smem = (pl.nt <= LN_TWO && !pl.pair ? 113 : 227) * 1024 - 2048 - (int)sizeof(LinearShared);
     p.stages = room_smem / stage_bytes;
     if (p.stages > LN_MAX_STAGES) p.stages = LN_MAX_STAGES;
     if (pl.splits > 1 && (size_t)p.stages * stage_bytes < (size_t)pl.nt * 512) return cudaErrorInvalidValue;   // (the parts of a split tile lie in the ring)
     const size_t smem = 1024 + (size_t)p.stages * stage_bytes + sizeof(LinearShared);
     const int per_cluster = (pl.pair ? 2 : 1) * pl.splits;
-    int64_t clusters = (pl.nt <= 64 && !pl.pair ? 2 : 1) * sms / per_cluster;
+    int64_t clusters = (pl.nt <= LN_TWO && !pl.pair ? 2 : 1) * sms / per_cluster;
     if (units < clusters) clusters = units;
     if (pl.splits > 1 && clusters < units) return cudaErrorInvalidValue;   // (a split tile is a cluster's only one)
 

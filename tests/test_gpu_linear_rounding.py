@@ -1,4 +1,4 @@
-"""16-bit results of cat_linear over long inner dimensions: how often they are the wrong neighbour of the exact value.
+"""cat_linear: 16-bit results over long inner dimensions, how often they are the wrong neighbour of the exact value; few tokens over many tiles.
 
 Tolerance, written down before the first run.  The tensor cores add 16 inner columns at a step and truncate the sum: a step drops ulp / 2 on
 average, 2^-24 * 0.72 of the sum's size (0.72: a number's mean distance above its binade's lower end).  Products of independent numbers make the
@@ -10,7 +10,7 @@ import pytest
 import torch
 
 from paper_2509_26277_b200 import binding as B
-from tests.test_gpu_linear import BF, FH, data
+from tests.test_gpu_linear import BF, F32, FH, check, data
 
 pytestmark = pytest.mark.gpu
 
@@ -24,3 +24,13 @@ def test_long_sums_round_to_the_nearest_neighbour(m, n, dtype, k):
     off = B.cat_linear(X, W).double() - exact.to(dtype).double()
     line = 1.3e-4 * (torch.finfo(dtype).eps / 2.0 ** -7) ** 0.5      # (fp16's steps are an eighth of bf16's)
     assert float(off.norm() / exact.norm()) < line
+
+
+@pytest.mark.parametrize("m", [9, 17, 32, 33, 64, 65])
+@pytest.mark.parametrize("n,k", [(19_000, 300), (40_000, 130)])
+def test_few_tokens_and_more_tiles_than_ctas(m, n, k):
+    """Single CTAs that take several tiles, one and two to an SM."""
+    X, W, g = data(m, n, k, FH)
+    residual = torch.randn((m, n), generator=g, device="cuda")
+    check(X, W, None, residual, "silu", F32, B.cat_linear(X, W, residual=residual, activation="silu", out_dtype=F32))
+    check(X, W, None, None, "none", FH, B.cat_linear(X, W))
