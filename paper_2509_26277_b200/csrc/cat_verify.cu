@@ -18,8 +18,9 @@
 //
 // A weight 2^(x c - M), c = log2(e) / T, M an integer: n = rint(x c), f = x c - n in two fused steps on c as a sum of two floats, 2^f
 // from the special function unit, n - M added to the exponent.  Its relative error does not grow with |x c|: f is off by at most
-// 2^-26 + 2^-26 + 2^-28 (two roundings of |f| <= 1/2, what c's two floats leave of |x c| <= 2^20), the unit's 2^f by 1.46e-7 of itself (the
-// largest over every float of [-0.51, 0.51], counted on the device): VF_EPS_WEIGHT.
+// 2^-26 + 2^-25 + 2^-28 (the roundings of x hi - n, at most 1/2, and of f, at most 1/2 + 2^-4, c's low float being worth up to 2^-4 where |x c| = 2^20; what
+// the two floats leave of x c), the unit's 2^f by 1.46e-7 of itself (the largest over every float of [-0.57, 0.57], counted on the device):
+// VF_EPS_WEIGHT.
 #include "cat_tc.cuh"
 
 #include <cuda_bf16.h>
@@ -134,7 +135,7 @@ constexpr int VF_EMPTY = -(1 << 28);                     // exponent of a part w
 constexpr int VF_WILD = 1 << 28;                         // exponent of a part that fp32 cannot hold (|x c| > 2^20)
 constexpr float VF_U = 5.9604645e-8f;                    // 2^-24
 // relative errors: of a weight; of the sum of a chunk (three roundings where a granule's weights are added, the rest in fp64); of a probability
-constexpr float VF_EPS_WEIGHT = 1.5e-7f + 0.6931472f * (2.f * 1.4901161e-8f + 3.7252903e-9f);
+constexpr float VF_EPS_WEIGHT = 1.46e-7f + 0.6931472f * (1.4901161e-8f + 2.9802322e-8f + 3.7252903e-9f);
 constexpr float VF_EPS_SUM = VF_EPS_WEIGHT + 3.f * VF_U;
 constexpr float VF_EPS_P = VF_EPS_WEIGHT + VF_EPS_SUM + 4.f * VF_U;
 
