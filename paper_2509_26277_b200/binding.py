@@ -535,6 +535,12 @@ def _control_block(index: int, stream: int) -> torch.Tensor:
     return ws
 
 
+def _own_workspace(ws: torch.Tensor, device: torch.device) -> torch.Tensor:
+    if ws.device != device or not ws.is_contiguous():
+        raise TypeError(f"ws must be a contiguous tensor on {device}")
+    return ws
+
+
 def _on_device(t: torch.Tensor, call, *args, **kwargs):
     """The call again with t's device current (the library launches on the current device)."""
     with torch.cuda.device(t.device):
@@ -608,6 +614,8 @@ def cat_linear(X, W, bias=None, residual=None, activation: str = "none", out=Non
             ws = torch.empty(max(256, L.cat_linear_workspace_bytes(x, ldx, w, ldw, M, N, K)), dtype=torch.uint8, device=device)
         else:
             ws = _control_block(index, stream)
+    else:
+        _own_workspace(ws, device)
     st = L.cat_linear(x, ldx, w, ldw, in_type, b, bias_type, r, ldr, act, M, N, K, out.data_ptr(), ldy, _TYPES[out_dtype],
                       ws.data_ptr(), ws.nbytes, stream)
     if st != CAT_OK:
@@ -675,6 +683,8 @@ def cat_verify_drafts(target, draft, draft_tokens, u_accept, u_sample, draft_len
     stream = torch._C._cuda_getCurrentRawStream(index)
     if ws is None:
         ws = _control_block(index, stream)
+    else:
+        _own_workspace(ws, device)
     st = (_lib or lib()).cat_verify_drafts(*t, *q, tokens, lengths, T, ua, us, B, S, V, out, kept, ws.data_ptr(), ws.nbytes, stream)
     if st != CAT_OK:
         raise CatError(st, "cat_verify_drafts")

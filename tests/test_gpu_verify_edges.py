@@ -168,3 +168,13 @@ def test_the_status_of_a_workspace_as_it_comes(b, v):
         if i == 0:
             once = B.cat_workspace_report(ws)["refined_rows_total"]
     assert B.cat_workspace_report(ws) == dict(B.cat_workspace_report(ws), device_status=0, refined_rows_total=3 * once)
+
+
+def test_workspaces_elsewhere_are_refused():
+    p = problem(2, 1, 100, BF, BF)
+    X, W = torch.zeros((4, 64), device="cuda", dtype=BF), torch.zeros((8, 64), device="cuda", dtype=BF)
+    for ws in (torch.zeros(256, dtype=torch.uint8), torch.zeros(512, dtype=torch.uint8, device="cuda")[::2], torch.zeros(1, device="cuda").expand(256)):
+        with pytest.raises(TypeError):
+            B.cat_verify_drafts(**p, ws=ws)
+        with pytest.raises(TypeError):
+            B.cat_linear(X, W, ws=ws)
