@@ -361,14 +361,13 @@ cat_status_t cat_apply_pca(const float *Yq, int64_t N, int32_t D, int32_t K, int
  * bias [N] of bias_type, may be NULL; residual may be NULL, or Y itself (with ldr = ldy).  Y shares no other memory with what is read (it may be
  * other columns of the same buffer, with rows as many bytes apart).
  * Rows are ldx, ldw, ldr, ldy elements apart (at least K, K, N, N; with one row its distance is not looked at); no base
- * address needs more alignment than its element.  Products are exact and sums formed in fp32 on the tensor cores, which truncate a sum
- * at every 16 inner columns where other fp32 sums round it (at most 768 columns, for a 16-bit out_type 1536, are added so before the next ones
- * are, rounded to nearest); bias, activation and residual in fp32 behind them, and the result is rounded once to out_type (overflow of fp16 gives
- * infinities).  Non-finite inputs
- * propagate as the arithmetic has it.  Activations:
+ * address needs more alignment than its element.  Products are exact and summed in fp32: by the tensor cores over up to 768 inner
+ * columns (a 16-bit out_type: 1536), truncating at every 16 of them, and these sums rounding to nearest.  Bias, activation and residual follow in fp32, and
+ * the result is rounded once to out_type (overflow of fp16 gives infinities).  Non-finite inputs propagate as the arithmetic has it.  Activations:
  *   CAT_ACT_RELU       max(z, 0)                     CAT_ACT_GELU       z Phi(z) (erf form)
  *   CAT_ACT_GELU_TANH  z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2          CAT_ACT_SILU  z / (1 + e^-z)
- * Results do not vary from run to run.  M = 0 does nothing.  Limits: M <= CAT_LINEAR_MAX_M, N and K <= CAT_LINEAR_MAX_N.
+ * Results do not vary from run to run.  M = 0 does nothing; N and K are at least 1.  Limits: M <= CAT_LINEAR_MAX_M, N and K <= CAT_LINEAR_MAX_N, ldx
+ * and ldw below 2^31, ldy and ldr <= CAT_LINEAR_MAX_LD.
  * Workspace: a control block; and where rows of X or W do not start on 16-byte boundaries (base or row distance), a copy
  * of that matrix is made there in every call.  A program that keeps weights for many calls keeps them with ldw a
  * multiple of 8.  The query only looks at the addresses.
@@ -380,6 +379,7 @@ cat_status_t cat_apply_pca(const float *Yq, int64_t N, int32_t D, int32_t K, int
 #define CAT_ACT_SILU 4
 #define CAT_LINEAR_MAX_M (1 << 24)
 #define CAT_LINEAR_MAX_N (1 << 20)
+#define CAT_LINEAR_MAX_LD ((int64_t)1 << 36)
 size_t cat_linear_workspace_bytes(const void *X, int64_t ldx, const void *W, int64_t ldw, int64_t M, int32_t N, int32_t K);
 cat_status_t cat_linear(const void *X, int64_t ldx, const void *W, int64_t ldw, int32_t in_type, const void *bias, int32_t bias_type,
                         const void *residual, int64_t ldr, int32_t activation, int64_t M, int32_t N, int32_t K,

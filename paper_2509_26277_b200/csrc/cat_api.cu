@@ -883,6 +883,7 @@ cat_status_t cat_linear(const void *X, int64_t ldx, const void *W, int64_t ldw, 
     if (activation < CAT_ACT_NONE || activation > CAT_ACT_SILU) return CAT_ERR_SHAPE;
     if (M > 1 && (ldy < N || (residual && ldr < N))) return CAT_ERR_SHAPE;
     if (M > 1 && residual == Y && residual && ldr != ldy) return CAT_ERR_SHAPE;
+    if (M > 1 && (ldy > CAT_LINEAR_MAX_LD || (residual && ldr > CAT_LINEAR_MAX_LD))) return CAT_ERR_UNSUPPORTED;   // (bytes of M rows fit 64 bits)
     if (M == 0) return CAT_OK;
     if (!X || !W || !Y) return CAT_ERR_NULL;
     if (misaligned(X, in_type) || misaligned(W, in_type) || misaligned(Y, out_type) || (residual && misaligned(residual, out_type)) ||

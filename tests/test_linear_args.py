@@ -61,3 +61,8 @@ def test_binding_refuses_cpu_tensors():
                                   dict(X=AT, ldx=128, W=AT + 65536, Y=AT + 256 * 7 + 64, ldy=100), dict(M=1, X=AT + 65536, W=AT + 128, Y=AT + 124, ldy=1)])
 def test_results_among_what_is_read_are_refused(over):
     assert call(**over) == 2
+
+
+@pytest.mark.parametrize("over", [dict(ldy=1 << 62), dict(ldy=(1 << 36) + 1), dict(residual=AT + (1 << 40), ldr=1 << 62), dict(M=2, ldy=(1 << 63) - 1)])
+def test_row_distances_whose_bytes_pass_64_bits_are_refused(over):
+    assert call(**dict(dict(Y=AT + (1 << 30)), **over)) == 7
