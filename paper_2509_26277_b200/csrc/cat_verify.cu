@@ -34,23 +34,8 @@ constexpr int VF_THREADS = 512;
 constexpr int VF_SETTLE_CLUSTER = 16;                      // (largest cluster there is)
 constexpr double VF_NO_RESIDUAL = 9.094947017729282e-13;   // 2^-40: a residual of less mass is what rounding left of none
 
-__device__ __forceinline__ uint32_t cta_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void sync_cluster()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 // address of the same shared-memory location in the CTA of the given rank
-__device__ __forceinline__ uint32_t peer(const void *p, uint32_t rank)
-{
-    uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
-    return a;
-}
+__device__ __forceinline__ uint32_t peer(const void *p, uint32_t rank) { return mapa_cluster((uint32_t)__cvta_generic_to_shared(p), rank); }
 __device__ __forceinline__ double peer_f64(const double *p, uint32_t rank)
 {
     double v;
@@ -709,7 +694,7 @@ struct Settle {
 
     __device__ Settle(const VerifyArgs &args, SettleShared &s, double *k, int n, double T) : a(args), sh(s), kept(k), size(n)
     {
-        rank = size > 1 ? (int)cta_rank() : 0;
+        rank = size > 1 ? (int)cluster_ctarank() : 0;
         warps = (int)blockDim.x >> 5;
         warp = threadIdx.x >> 5;
         lane = threadIdx.x & 31;
@@ -748,7 +733,7 @@ struct Settle {
             const double s = warp_sum(lane < warps ? sh.part[warp][lane] : 0.0);
             if (lane == 0) sh.cta[turn][warp] = s;
         }
-        sync_cluster();
+        cluster_sync();
         v0 = warp_sum(lane < size ? peer_f64(&sh.cta[turn][0], (uint32_t)lane) : 0.0);
         v1 = warp_sum(lane < size ? peer_f64(&sh.cta[turn][1], (uint32_t)lane) : 0.0);
     }
@@ -838,7 +823,7 @@ struct Settle {
             const float t = warp_max(lane < warps ? sh.top[lane] : -CUDART_INF_F);
             if (lane == 0) sh.cta_top[top_turn] = t;
         }
-        sync_cluster();
+        cluster_sync();
         return warp_max(lane < size ? peer_f32(&sh.cta_top[top_turn], (uint32_t)lane) : -CUDART_INF_F);
     }
 };
@@ -962,7 +947,7 @@ __device__ __noinline__ void settle_sequence(const VerifyParams &p, SettleShared
         for (int k = j + 1 + (int)threadIdx.x; k <= a.S; k += (int)blockDim.x) out[k] = -1;
         if (threadIdx.x == 0) a.accepted_out[b] = j;
     }
-    sync_cluster();   // (everything shared has been read)
+    cluster_sync();   // (everything shared has been read)
 }
 
 // The sequences that verify_kernel left undecided (accepted_out[b] = -2 - row to go on from).  A cluster claims one after the other -- who
@@ -977,7 +962,7 @@ __global__ void __launch_bounds__(VF_THREADS, 1) verify_settle_kernel(const __gr
     pdl_enter();
     const VerifyArgs &a = p.a;
     const int clusters = (int)gridDim.x / p.size, own = (int)blockIdx.x / p.size, lane = threadIdx.x & 31;
-    const bool chooses = cta_rank() == 0 && threadIdx.x < 32;
+    const bool chooses = cluster_ctarank() == 0 && threadIdx.x < 32;
     const int64_t start = (int64_t)a.B * own / clusters;
     int64_t looked = 0;
     for (;;) {
@@ -1006,12 +991,12 @@ __global__ void __launch_bounds__(VF_THREADS, 1) verify_settle_kernel(const __gr
                 if (claim >= 0) sh.head = read_head(a, claim);
             }
         }
-        sync_cluster();
+        cluster_sync();
         const int b = peer_s32(&sh.claim[0], 0), row = peer_s32(&sh.claim[1], 0);
         if (b < 0) break;
         settle_sequence<TT, QT>(p, sh, p.keep ? kept : nullptr, p.size, b, row, peer_head(&sh.head, 0));      // (its barriers lie between this claim's reading and the next one's writing)
     }
-    sync_cluster();
+    cluster_sync();
 }
 
 template <int TT, int QT, int VECS>
@@ -1023,16 +1008,16 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
     const VerifyArgs &a = p.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = (int)blockDim.x >> 5;
     const int size = p.size;
-    const uint32_t rank = size > 1 ? cta_rank() : 0u;
+    const uint32_t rank = size > 1 ? cluster_ctarank() : 0u;
     const int b = (int)blockIdx.x / size;
     if (blockIdx.x == 0 && tid == 0) p.ctl->device_status = CAT_OK;      // (nothing here waits for long)
     if (rank == 0 && tid == 0) sh.head = read_head(a, b);
-    if (size > 1) sync_cluster();
+    if (size > 1) cluster_sync();
     else __syncthreads();
     const Head head = peer_head(&sh.head, 0);
     const int length = head.length;
     if (length < 0) {                       // (all CTAs of the cluster)
-        if (size > 1) sync_cluster();       // (all have read the first one's shared memory)
+        if (size > 1) cluster_sync();       // (all have read the first one's shared memory)
         return;
     }
     const bool greedy = !(head.T > 0.f), decides = warp == warps - 1, drafts = a.draft != nullptr && !greedy;
@@ -1125,7 +1110,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
             }
         }
         if (size > 1) {
-            sync_cluster();
+            cluster_sync();
             for (int r = warp; r < rows; r += warps) {
                 double z = lane < size ? peer_f64(&sh.row_z[turn][r], (uint32_t)lane) : no_z;
                 int m = lane < size ? peer_s32(&sh.row_m[turn][r], (uint32_t)lane) : no_m;
@@ -1267,7 +1252,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
                         sh.row_m[turn][0] = mt;
                     }
                 }
-                if (size > 1) sync_cluster();
+                if (size > 1) cluster_sync();
             }
             if (warp == 0) {
                 // the CTA, the chunk, the entry at which the sum passes u times the whole
@@ -1308,11 +1293,11 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(const __grid_cons
     if (verdict == VF_UNDECIDED && rank == 0 && tid == 0) a.accepted_out[b] = -2 - j;
     if (rank == 0)
         for (int k = j + 1 + tid; k <= a.S; k += (int)blockDim.x) out[k] = -1;
-    if (size > 1) sync_cluster();   // no CTA's shared memory goes away under another
+    if (size > 1) cluster_sync();   // no CTA's shared memory goes away under another
     else __syncthreads();
     if (p.settle) {
         const bool open = verdict == VF_UNDECIDED || peer_s32(&sh.open, (uint32_t)sh.owner) != 0;
-        if (size > 1) sync_cluster();
+        if (size > 1) cluster_sync();
         if (open) {
             fill_table(sh.settle.table);
             __syncthreads();
