@@ -10,11 +10,12 @@
 // 16-byte granules (one or four per lane, in flight together).  A chunk leaves its largest exponent (an integer in units of log 2) and its
 // sum of weights, so one read of a row gives its normaliser and, where the row itself is drawn from, the chunk that holds the token; only a
 // residual reads its two rows again, out of L2.  `group` rows and their drafts go through between two exchanges: few where reading the rows
-// behind a refusal for nothing costs more than an exchange, up to eight where it does not.  What bounds it: a small batch the chain of load,
-// sums, exchange, decision and draw (8 sequences of 4 drafts over 32 000: 15 us, the bytes 2.8); a large one the instructions, about twelve an entry
-// (256 rows of 50 001: 17 us, 1.5 TB/s; 64 sequences of 7 drafts over 128 000: 70 us for the 130 MB that it reads).
+// behind a refusal for nothing costs more than an exchange, up to eight where it does not.  What bounds it: the latency of a
+// sequence's phases -- load, sums, exchange, decision, draw -- one after the other (8 sequences of 4 drafts over 32 000: 16 us, the bytes 2.8); with a large
+// batch that of its loads too, which stop between the phases (cold, alone: 256 rows of 50 001 25 us at 0.25 instructions a cycle and scheduler; 64
+// sequences of 7 drafts over 128 000 84 us for the 130 MB that it reads, 0.45).
 //
-// verify_settle_kernel, and the same in verify_kernel: what the sums leave undecided, in fp64.  Bound by latency: 12 us a sequence of 32 000.
+// verify_settle_kernel, and the same in verify_kernel: what the sums leave undecided, in fp64.  Bound by latency: 14 us a sequence of 32 000.
 //
 // A weight 2^(x c - M), c = log2(e) / T, M an integer: n = rint(x c), f = x c - n in two fused steps on c as a sum of two floats, 2^f
 // from the special function unit, n - M added to the exponent.  Its relative error does not grow with |x c|: f is off by at most
@@ -1343,8 +1344,8 @@ cudaError_t launch_verify(const VerifyArgs &a, void *workspace, cudaStream_t s)
     p.size = 1;
     while (p.size < 8 && (int64_t)a.B * p.size <= sms && entries >= 1024 * p.size) p.size *= 2;
     while (p.size < 8 && entries > (int64_t)(1 << 19) * p.size) p.size *= 2;
-    // One granule per lane and chunk where no SM has a second CTA to hide a long chunk's latency behind (8 sequences, 4 drafts, V = 32 000: 15 us
-    // against 17); four, with a quarter of the sums over the warp, where it has (64 sequences, 7 drafts, V = 128 000: 132 us against 186).
+    // One granule per lane and chunk where no SM has a second CTA to hide a long chunk's latency behind (8 sequences, 4 drafts, V = 32 000: 16 us
+    // against 19); four, with a quarter of the sums over the warp, where it has (64 sequences, 7 drafts, V = 128 000: 107 us against 164).
     p.vecs = (int64_t)a.B * p.size <= sms ? 1 : 4;
     auto chunks = [&](int type) {
         const int per = type == CAT_F32 ? 4 : 8, chunk = 32 * p.vecs * per;
@@ -1362,7 +1363,7 @@ cudaError_t launch_verify(const VerifyArgs &a, void *workspace, cudaStream_t s)
     if (p.group > p.max_group) p.group = p.max_group;
     p.slots = p.max_group * (per_t + per_q);
     // An undecided sequence is settled by the CTAs that have it where every thread has sixteen entries of a row at most; else by a cluster of 16 in a
-    // launch of its own (64 sequences, V = 128 000: 116 us against 142; 256 sequences, V = 50 001: 39 us against 88).
+    // launch of its own (64 sequences, V = 128 000: 107 us against 143; 256 sequences, V = 50 001: 32 us against 61).
     p.settle = entries <= (int64_t)16 * VF_THREADS * p.size;
     // (the weights of two rows in fp64: where a CTA has an SM to itself, or they are small)
     auto kept_bytes = [&](int size) { return ((entries + 6) / 4 / size + 1) * 64; };
